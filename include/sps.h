@@ -57,6 +57,9 @@ typedef enum {
  * (Modified Rejection Sampling section); this is the library's definition
  * for inputs that are not. */
 #define SPS_DEV_NONFINITE 8
+/* A page-table entry outside [0, n_pages) for a position that a call writes
+ * (the write is skipped) or reads (its page is not attended to). */
+#define SPS_DEV_BAD_PAGE 16
 
 enum { SPS_FFN_GELU = 0, SPS_FFN_SWIGLU = 1 };
 enum { SPS_DTYPE_F32 = 0, SPS_DTYPE_BF16 = 1, SPS_DTYPE_FP8 = 2 };
@@ -327,6 +330,125 @@ sps_status sps_philox_uniforms(sps_philox rng, int32_t purpose, int32_t B, int32
  * feeds to acceptance. */
 sps_status sps_softmax(const float* logits, int32_t rows, int32_t V, sps_sampling sampling,
                        float* probs, void* stream);
+
+/* ---- rotary positions ------------------------------------------------- */
+
+/* Rotary position encoding of the first rot_dim dims of every head (even,
+ * 2 .. head_dim); the dims behind them are passed through. Pair i < rot_dim / 2
+ * is dims (i, i + rot_dim / 2) (HALF) or (2 i, 2 i + 1) (INTERLEAVED), and at
+ * position p (a, b) becomes A (a cos t - b sin t, a sin t + b cos t) with
+ * t = p f_i, A = amplitude, f_i = base^(-2 i / rot_dim). factor > 1 stretches
+ * the positions for contexts longer than the model's own:
+ *   original_len == 0: f_i / factor for every pair (linear interpolation);
+ *   original_len  > 0: f_i (g + (1 - g) / factor), interpolation by parts
+ *     (Peng et al. 2023): g goes from 0 to 1 as the turns the pair makes in
+ *     the original context, original_len f_i / (2 pi), go from low_turns to
+ *     high_turns (0 <= low_turns < high_turns).
+ * Angles are computed in fp64, so far positions keep their precision. base
+ * > 0, factor > 0; every value finite. */
+enum { SPS_ROPE_HALF = 0, SPS_ROPE_INTERLEAVED = 1 };
+typedef struct {
+  int32_t rot_dim, layout;
+  float base, factor;
+  int32_t original_len;
+  float low_turns, high_turns, amplitude;
+} sps_rope_spec;
+
+/* out[r][h][:] = the rotation of x[r][h][:] at position positions[r], or with
+ * backward != 0 its transpose (the gradient with respect to x of a loss whose
+ * gradient with respect to the rotated heads is x). x and out are [rows][heads][head_dim] of
+ * dtype SPS_DTYPE_F32 or _BF16, their rows x_stride and out_stride elements
+ * apart (at least heads * head_dim). out may be x (with the same stride) and
+ * must not overlap it otherwise. head_dim is even, 2 .. 256; heads 1 .. 1024;
+ * rows 0 .. 2^24. The keys sps_kv_write takes are rotated by this. */
+sps_status sps_rope(const void* x, int64_t x_stride, const int32_t* positions, const sps_rope_spec* spec,
+                    int32_t rows, int32_t heads, int32_t head_dim, int32_t dtype, int32_t backward, void* out,
+                    int64_t out_stride, void* stream);
+
+/* ---- paged KV cache ---------------------------------------------------- */
+
+/* A KV cache in pages of page_size positions that sequences of a batch take
+ * as they grow: position p of sequence b is position p % page_size of page
+ * page_table[b][p / page_size]. n_heads query heads share n_kv_heads KV heads
+ * (query head h reads KV head h / (n_heads / n_kv_heads)).
+ * Supported: head_dim in {64, 128}, dtype SPS_DTYPE_F32 or _BF16, page_size a
+ * power of two in [32, 1024], 1 <= n_kv_heads <= n_heads <= 1024 with n_heads %
+ * n_kv_heads == 0, 1 <= B <= 1024, max_pages * page_size <= 2^22, 1 <=
+ * n_pages <= 2^24, 1 <= n_layers <= 4096, the whole cache at most 2^50 bytes.
+ *
+ * Layout: per layer a key plane, then a value plane, each
+ * [n_pages][n_kv_heads][page_size * head_dim]. Within a page and head, keys
+ * are 16-position x 32-dim tiles, element (p, d) at
+ *   ((p/16 * (head_dim/32) + d/32) * 64 + p%16 + 16 (d%32 / 8)) * 8 + d%8,
+ * and values 32-position x 16-dim tiles, with w = p % 32 at
+ *   ((p/32 * (head_dim/16) + d/16) * 64 + d%16 + 16 (w%16 / 4)) * 8 + 4 (w/16) + w%4:
+ * the tiles of sps_kv_bytes' cache, which a page thus holds 16 or 32
+ * positions at a time. */
+typedef struct {
+  int32_t n_heads, n_kv_heads, head_dim, dtype;
+  int32_t n_layers, n_pages, page_size;
+  int32_t B, max_pages;
+} sps_paged_config;
+
+typedef struct sps_paged_s* sps_paged_t;
+
+/* Bytes of the cache buffer (0 if cfg is invalid). */
+size_t sps_paged_bytes(const sps_paged_config* cfg);
+
+/* Create a handle over `buf` (sps_paged_bytes bytes, 256-byte aligned),
+ * `page_table` (device int32 [B][max_pages]; entries that no position below
+ * a sequence's length needs are not read) and `lengths` (device int32 [B],
+ * committed lengths, as for sps_kv_create, whose array it may be). The caller
+ * initialises and updates both arrays. SPS_E_SHAPE for an invalid cfg. */
+sps_status sps_paged_create(const sps_paged_config* cfg, void* buf, const int32_t* page_table,
+                            const int32_t* lengths, sps_paged_t* out /*host*/);
+void sps_paged_destroy(sps_paged_t kv);
+
+/* The rows of a call: `rows` new tokens of the cache's B sequences, one
+ * sequence after the other, at most max_tokens of one sequence. Sequence b has
+ * rows starts[b] .. starts[b + 1] - 1 (device int32 [B + 1], non-decreasing,
+ * none of them outside [0, rows]; a sequence may have none, and rows before
+ * the first and behind the last sequence's are neither read nor written), or with
+ * starts == NULL rows b max_tokens .. (b + 1) max_tokens - 1, and rows is B
+ * max_tokens. Row j of its sequence sits at position lengths[b] + pos_offset + j;
+ * lengths are not advanced. Starts that break these rules set
+ * SPS_DEV_CAPACITY, and what the rows of their sequences get is not defined.
+ * rows <= 2^20; strides are elements from row to row. */
+
+/* Write the new tokens' keys and values ([rows][n_kv_heads][head_dim], the
+ * cache's dtype) into their pages of layer `layer`, the keys rotated by
+ * `rope` (NULL: as they are). If q != NULL the queries ([rows][n_heads]
+ * [head_dim]) are rotated alike into q_out, which may be q with the same stride.
+ * A position outside [0, max_pages page_size) is skipped and sets
+ * SPS_DEV_CAPACITY, one on a bad page SPS_DEV_BAD_PAGE; positions not named
+ * keep their contents. Two sequences must not append to one page. */
+sps_status sps_paged_append(sps_paged_t kv, int32_t layer, const void* k, int64_t k_stride, const void* v,
+                            int64_t v_stride, const sps_rope_spec* rope, const void* q, int64_t q_stride,
+                            void* q_out, int64_t q_out_stride, const int32_t* starts, int32_t rows,
+                            int32_t max_tokens, int32_t pos_offset, void* stream);
+
+/* Bytes of scratch sps_paged_attention needs for up to `rows` rows with at
+ * most max_tokens of one sequence (0 for a request it does not admit); one
+ * for more rows or tokens also fits. */
+size_t sps_paged_workspace_bytes(const sps_paged_config* cfg, int32_t rows, int32_t max_tokens);
+
+/* Attention of the new tokens over the pages of their sequences: out[r][h] =
+ * sum_p w_p V[p] with w the softmax of scale q[r][h] . K[p] over the
+ * positions p <= the row's own position, no more than `window` of them
+ * (window == 0: all), below max_pages page_size and on good pages (a bad one
+ * sets SPS_DEV_BAD_PAGE). The new tokens' own keys and values have to be in
+ * the cache (sps_paged_append). Positions a row does not see have no effect
+ * on it, whatever they hold. A row that sees none, or whose scores are all
+ * -Inf, gets zeros. lse, if not NULL, fp32 [rows][n_heads]: the natural log
+ * of the sum of exp(scale q . K) (-Inf for a row of zeros), with which
+ * results over several caches can be joined. q and out are [rows][n_heads][head_dim] of the
+ * cache's dtype; scale > 0 and finite. The scores, the softmax and its
+ * sums are fp32. `workspace` is 256-byte aligned; its contents carry nothing
+ * from call to call. */
+sps_status sps_paged_attention(sps_paged_t kv, int32_t layer, const void* q, int64_t q_stride,
+                               const int32_t* starts, int32_t rows, int32_t max_tokens, int32_t pos_offset,
+                               float scale, int32_t window, void* out, int64_t out_stride, float* lse,
+                               void* workspace, size_t ws_bytes, void* stream);
 
 /* Measurement helpers. Between begin and end, every weight-streaming GEMM
  * launch (the linear layers: QKV, attention output, FFN, unembedding) is

@@ -80,6 +80,37 @@ hipError_t launch_attention(int dtype, const void* q, const void* kc, const void
 hipError_t launch_kv_copy(int dtype, int to_cache, void* kc, void* vc, int H, int DH, int T_cap,
                           int pos0, int n, void* k, void* v, hipStream_t st);
 
+// Rotary positions (rope.hip). Frequencies in turns per position, computed on
+// the device in fp64: f_i = exp2(step i) / (2 pi), stretched by inv_factor
+// (linear) or by parts.
+struct RopeArgs {
+  int rot, interleaved, by_parts;
+  float amp;
+  double step, inv_factor, original, low, inv_span;
+};
+RopeArgs rope_args(const sps_rope_spec& r);
+hipError_t launch_rope(int dtype, const void* x, int64_t ldx, const int32_t* positions, const RopeArgs& r, int rows,
+                       int heads, int DH, bool backward, void* out, int64_t ldo, hipStream_t st);
+
+// The paged cache (paged.hip, paged_attention.hip): one layer's planes and
+// what finds a position in them, and the rows of a call (see sps.h).
+struct PagedView {
+  void *k, *v;
+  const int32_t *table, *lengths;
+  int H, G, DH;                          // KV heads, query heads per KV head
+  int n_pages, page_log2, max_pages, B;
+};
+struct PagedRows {
+  const int32_t* starts;                 // NULL: max_tokens rows of every sequence
+  int rows, max_tokens, pos_offset;
+};
+hipError_t launch_paged_append(int dtype, const PagedView& c, const PagedRows& r, const void* k, int64_t ldk,
+                               const void* v, int64_t ldv, const RopeArgs* rope, const void* q, int64_t ldq, void* qo,
+                               int64_t ldqo, int* err, hipStream_t st);
+hipError_t launch_paged_attention(int dtype, const PagedView& c, const PagedRows& r, const PagedPlan& p, const void* q,
+                                  int64_t ldq, float scale, int window, void* out, int64_t ldo, float* lse,
+                                  float* part_o, float2* part_ml, int* err, hipStream_t st);
+
 // Sampling.
 // Row statistics (stats, row_stat_bytes() each, may be NULL) and, if probs
 // != NULL, the probabilities after temperature and the top-k / nucleus

@@ -3,6 +3,7 @@
 #include "plan.h"
 
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 
 namespace sps {
@@ -234,6 +235,87 @@ size_t prefill_workspace_bytes(const sps_config* cfg, int B, int tokens, int T_c
   if (!valid_config(cfg) || B < 1 || tokens < 1 || T_cap < 32 || T_cap > kMaxTCap) return 0;
   if (static_cast<long>(B) * tokens > kMaxRows) return 0;
   return make_ws(make_layout(cfg), B, tokens, T_cap).total;
+}
+
+// ---- rotary positions and the paged cache --------------------------------
+
+bool valid_rope(const sps_rope_spec* r, int head_dim) {
+  if (!r) return false;
+  if (r->rot_dim < 2 || r->rot_dim % 2 || r->rot_dim > head_dim) return false;
+  if (r->layout != SPS_ROPE_HALF && r->layout != SPS_ROPE_INTERLEAVED) return false;
+  if (!(r->base > 0.f) || !std::isfinite(r->base) || !(r->factor > 0.f) || !std::isfinite(r->factor)) return false;
+  if (!std::isfinite(r->amplitude) || r->original_len < 0) return false;
+  if (r->original_len > 0 && (!(r->low_turns >= 0.f) || !(r->high_turns > r->low_turns) || !std::isfinite(r->high_turns)))
+    return false;
+  return true;
+}
+
+bool valid_paged(const sps_paged_config* c) {
+  if (!c) return false;
+  if (c->dtype != SPS_DTYPE_F32 && c->dtype != SPS_DTYPE_BF16) return false;
+  if (c->head_dim != 64 && c->head_dim != 128) return false;
+  if (c->n_kv_heads < 1 || c->n_heads < c->n_kv_heads || c->n_heads > 1024 || c->n_heads % c->n_kv_heads) return false;
+  if (c->page_size < 32 || c->page_size > 1024 || (c->page_size & (c->page_size - 1))) return false;
+  if (c->n_layers < 1 || c->n_layers > 4096 || c->n_pages < 1 || c->n_pages > (1 << 24)) return false;
+  if (c->B < 1 || c->B > kMaxPagedB || c->max_pages < 1 || c->max_pages > kMaxTCap / c->page_size) return false;
+  // Elements: n_pages page_size <= 2^34, heads x dim <= 2^17, 2 layers <= 2^13: at
+  // most 2^64, so the limit is applied to the factors.
+  const double bytes = 2.0 * c->n_layers * static_cast<double>(paged_plane_elems(*c)) * (c->dtype == SPS_DTYPE_F32 ? 4 : 2);
+  return bytes <= 1125899906842624.0;   // 2^50
+}
+
+size_t paged_plane_elems(const sps_paged_config& c) {
+  return static_cast<size_t>(c.n_pages) * c.n_kv_heads * c.page_size * c.head_dim;
+}
+
+size_t paged_bytes(const sps_paged_config* c) {
+  if (!valid_paged(c)) return 0;
+  return static_cast<size_t>(2) * c->n_layers * paged_plane_elems(*c) * (c->dtype == SPS_DTYPE_F32 ? 4 : 2);
+}
+
+sps_status check_paged_rows(const sps_paged_config& c, bool ragged, int rows, int max_tokens) {
+  if (rows < 0 || max_tokens < 0) return SPS_E_INVALID;
+  if (rows > kMaxPagedRows || max_tokens > kMaxPagedRows) return SPS_E_SHAPE;
+  if (rows > 0 && max_tokens == 0) return SPS_E_INVALID;
+  if (!ragged && static_cast<long>(c.B) * max_tokens != rows) return SPS_E_INVALID;
+  return SPS_OK;
+}
+
+PagedPlan paged_plan(const sps_paged_config& c, int rows, int max_tokens) {
+  PagedPlan p{};
+  const int G = c.n_heads / c.n_kv_heads;
+  const long q = static_cast<long>(std::min(rows, max_tokens)) * G;
+  p.qt = q <= 16 ? 1 : 2;
+  p.target = 4 * kCUs;
+  const long tile = 16L * p.qt;
+  // Every sequence's last tile may be partly filled.
+  const long tiles = (static_cast<long>(rows) * G / tile + std::min(c.B, rows)) * c.n_kv_heads;
+  const long blocks = (static_cast<long>(c.max_pages) * c.page_size) / 32;
+  const long ranges = (blocks + kPagedMinBlocks - 1) / kPagedMinBlocks;
+  // A sequence of n blocks has at most n / per + 1 ranges, and per is at least
+  // (all tiles' blocks) / target, so the ranges are at most target plus one a
+  // tile; only tiles of two ranges or more leave partials, at most twice
+  // their n / per.
+  p.items = std::min(tiles * ranges, tiles + p.target);
+  p.slots = ranges > 1 ? std::min(p.items, 2L * p.target) : 0;
+  p.joins = std::min(tiles, p.slots / 2);
+  p.o_off = 0;
+  p.ml_off = align256(static_cast<size_t>(p.slots) * tile * c.head_dim * 4);
+  p.total = p.ml_off + align256(static_cast<size_t>(p.slots) * tile * 8);
+  if (p.total == 0) p.total = 256;
+  return p;
+}
+
+size_t paged_workspace_bytes(const sps_paged_config* c, int rows, int max_tokens) {
+  if (!valid_paged(c) || rows < 0 || max_tokens < 0 || rows > kMaxPagedRows || max_tokens > kMaxPagedRows ||
+      (rows > 0 && max_tokens == 0))
+    return 0;
+  // Calls with fewer tokens per sequence have smaller tiles and may have more of them.
+  size_t most = 256;
+  const int G = c->n_heads / c->n_kv_heads;
+  for (long q : {16L, static_cast<long>(kMaxPagedRows)})
+    most = std::max(most, paged_plan(*c, rows, static_cast<int>(std::max(1L, std::min<long>(max_tokens, q / G)))).total);
+  return most;
 }
 
 sps_status check_sampling(const sps_sampling& sp, int V) {

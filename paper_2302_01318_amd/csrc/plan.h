@@ -176,6 +176,38 @@ void cut_segments(int rows, int V, int* seg, int* nseg);
 // Bytes of split-K partials the launches of one forward over M rows write.
 size_t forward_part_bytes(const Layout& L, int M);
 
+// ---- rotary positions and the paged cache --------------------------------
+constexpr int kMaxRopeDim = 256;       // head_dim of sps_rope
+constexpr int kMaxRopeRows = 1 << 24;
+constexpr int kMaxPagedB = 1024;       // sequences: the kernels keep a word or two per sequence in LDS
+constexpr int kMaxPagedRows = 1 << 20;
+
+bool valid_rope(const sps_rope_spec* r, int head_dim);
+bool valid_paged(const sps_paged_config* c);
+size_t paged_plane_elems(const sps_paged_config& c);   // elements of one key or value plane of a layer
+size_t paged_bytes(const sps_paged_config* c);
+// Whether a call's rows are ones the paged operators take (starts: ragged).
+sps_status check_paged_rows(const sps_paged_config& c, bool ragged, int rows, int max_tokens);
+
+// Attention over the pages. A work item is the tile of up to `tile` query
+// rows (a sequence's tokens x the query heads of one KV head) against a range
+// of 32-position blocks. Ranges are the same number of blocks for the whole
+// call, chosen on the device from the actual lengths so that there are about
+// `target` items, no fewer than kPagedMinBlocks each. Items whose rows have only one range
+// write the output; the others leave partials in at most `slots` slots of the
+// workspace, which a second launch joins.
+constexpr int kPagedMinBlocks = 8;     // 256 positions: two blocks per wave
+struct PagedPlan {
+  int qt;              // 16-row tiles per item
+  int target;          // items wanted
+  long items;          // most items there can be: the grid
+  long slots;          // most partials there can be
+  long joins;          // most (tile, KV head) pairs with partials
+  size_t o_off, ml_off, total;   // workspace: partial outputs, then (max, sum) pairs
+};
+PagedPlan paged_plan(const sps_paged_config& c, int rows, int max_tokens);
+size_t paged_workspace_bytes(const sps_paged_config* c, int rows, int max_tokens);
+
 // Host-side check of the sampling parameters for a vocabulary of V.
 sps_status check_sampling(const sps_sampling& sp, int V);
 

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <new>
 #include <vector>
@@ -79,7 +80,34 @@ struct sps_kv_s {
   size_t plane_bytes;  // one of K or V for one layer: B * H * T_cap * DH elements
 };
 
+struct sps_paged_s {
+  sps_paged_config cfg;
+  char* buf;
+  const int32_t *table, *lengths;
+};
+
 namespace {
+
+sps::PagedView paged_view(const sps_paged_s* kv, int layer) {
+  const sps_paged_config& c = kv->cfg;
+  const size_t plane = sps::paged_plane_elems(c) * (c.dtype == SPS_DTYPE_F32 ? 4 : 2);
+  sps::PagedView w{};
+  w.k = kv->buf + plane * (2 * static_cast<size_t>(layer));
+  w.v = kv->buf + plane * (2 * static_cast<size_t>(layer) + 1);
+  w.table = kv->table;
+  w.lengths = kv->lengths;
+  w.H = c.n_kv_heads;
+  w.G = c.n_heads / c.n_kv_heads;
+  w.DH = c.head_dim;
+  w.n_pages = c.n_pages;
+  w.page_log2 = __builtin_ctz(static_cast<unsigned>(c.page_size));
+  w.max_pages = c.max_pages;
+  w.B = c.B;
+  return w;
+}
+// Row strides of the caller's tensors: whole rows, and offsets that stay inside 64 bits.
+bool good_stride(int64_t stride, int64_t width) { return stride >= width && stride <= (int64_t{1} << 36); }
+bool misaligned(const void* p, int dtype) { return reinterpret_cast<uintptr_t>(p) % (dtype == SPS_DTYPE_F32 ? 4 : 2) != 0; }
 
 char* layer_ptr(const sps_model_s* m, int l, size_t off) {
   return m->base + m->L.layer0 + m->L.layer_stride * l + off;
@@ -601,6 +629,103 @@ sps_status sps_softmax(const float* logits, int32_t rows, int32_t V, sps_samplin
   if (!err) return SPS_E_HIP;
   SPS_HIP(sps::launch_softmax(logits, rows, V, sampling.temperature, sampling.top_k, sampling.top_p, probs, err,
                               as_stream(stream)));
+  return SPS_OK;
+}
+
+sps_status sps_rope(const void* x, int64_t x_stride, const int32_t* positions, const sps_rope_spec* spec, int32_t rows,
+                    int32_t heads, int32_t head_dim, int32_t dtype, int32_t backward, void* out, int64_t out_stride,
+                    void* stream) {
+  if (rows < 0 || heads < 1 || head_dim < 2 || head_dim % 2) return SPS_E_INVALID;
+  if (rows > sps::kMaxRopeRows || heads > 1024 || head_dim > sps::kMaxRopeDim) return SPS_E_SHAPE;
+  if (dtype != SPS_DTYPE_F32 && dtype != SPS_DTYPE_BF16) return SPS_E_UNSUPPORTED;
+  if (!sps::valid_rope(spec, head_dim)) return SPS_E_INVALID;
+  if (!good_stride(x_stride, heads * head_dim) || !good_stride(out_stride, heads * head_dim)) return SPS_E_INVALID;
+  if (rows == 0) return SPS_OK;
+  if (!x || !out || !positions || (x == out && x_stride != out_stride)) return SPS_E_INVALID;
+  if (misaligned(x, dtype) || misaligned(out, dtype)) return SPS_E_INVALID;
+  SPS_HIP(sps::launch_rope(dtype, x, x_stride, positions, sps::rope_args(*spec), rows, heads, head_dim, backward != 0,
+                           out, out_stride, as_stream(stream)));
+  return SPS_OK;
+}
+
+size_t sps_paged_bytes(const sps_paged_config* cfg) { return sps::paged_bytes(cfg); }
+
+sps_status sps_paged_create(const sps_paged_config* cfg, void* buf, const int32_t* page_table, const int32_t* lengths,
+                            sps_paged_t* out) {
+  if (!out) return SPS_E_INVALID;
+  *out = nullptr;
+  if (!sps::valid_paged(cfg)) return SPS_E_SHAPE;
+  if (!buf || !page_table || !lengths || reinterpret_cast<uintptr_t>(buf) % 256) return SPS_E_INVALID;
+  sps_paged_s* kv = new (std::nothrow) sps_paged_s;
+  if (!kv) return SPS_E_CAPACITY;
+  kv->cfg = *cfg;
+  kv->buf = static_cast<char*>(buf);
+  kv->table = page_table;
+  kv->lengths = lengths;
+  *out = kv;
+  return SPS_OK;
+}
+
+void sps_paged_destroy(sps_paged_t kv) { delete kv; }
+
+sps_status sps_paged_append(sps_paged_t kv, int32_t layer, const void* k, int64_t k_stride, const void* v,
+                            int64_t v_stride, const sps_rope_spec* rope, const void* q, int64_t q_stride, void* q_out,
+                            int64_t q_out_stride, const int32_t* starts, int32_t rows, int32_t max_tokens,
+                            int32_t pos_offset, void* stream) {
+  if (!kv) return SPS_E_INVALID;
+  const sps_paged_config& c = kv->cfg;
+  if (layer < 0 || layer >= c.n_layers) return SPS_E_INVALID;
+  const sps_status s = sps::check_paged_rows(c, starts != nullptr, rows, max_tokens);
+  if (s != SPS_OK) return s;
+  if (rope && !sps::valid_rope(rope, c.head_dim)) return SPS_E_INVALID;
+  const int kvw = c.n_kv_heads * c.head_dim, qw = c.n_heads * c.head_dim;
+  if (!good_stride(k_stride, kvw) || !good_stride(v_stride, kvw)) return SPS_E_INVALID;
+  if ((q == nullptr) != (q_out == nullptr)) return SPS_E_INVALID;
+  if (q && (!good_stride(q_stride, qw) || !good_stride(q_out_stride, qw) || (q == q_out && q_stride != q_out_stride)))
+    return SPS_E_INVALID;
+  if (rows == 0) return SPS_OK;
+  if (!k || !v || misaligned(k, c.dtype) || misaligned(v, c.dtype) || misaligned(q, c.dtype) ||
+      misaligned(q_out, c.dtype))
+    return SPS_E_INVALID;
+  int* err = device_error_ptr();
+  if (!err) return SPS_E_HIP;
+  sps::RopeArgs ra{};
+  if (rope) ra = sps::rope_args(*rope);
+  SPS_HIP(sps::launch_paged_append(c.dtype, paged_view(kv, layer), {starts, rows, max_tokens, pos_offset}, k, k_stride,
+                                   v, v_stride, rope ? &ra : nullptr, q, q_stride, q_out, q_out_stride, err,
+                                   as_stream(stream)));
+  return SPS_OK;
+}
+
+size_t sps_paged_workspace_bytes(const sps_paged_config* cfg, int32_t rows, int32_t max_tokens) {
+  return sps::paged_workspace_bytes(cfg, rows, max_tokens);
+}
+
+sps_status sps_paged_attention(sps_paged_t kv, int32_t layer, const void* q, int64_t q_stride, const int32_t* starts,
+                               int32_t rows, int32_t max_tokens, int32_t pos_offset, float scale, int32_t window,
+                               void* out, int64_t out_stride, float* lse, void* workspace, size_t ws_bytes,
+                               void* stream) {
+  if (!kv) return SPS_E_INVALID;
+  const sps_paged_config& c = kv->cfg;
+  if (layer < 0 || layer >= c.n_layers || window < 0) return SPS_E_INVALID;
+  if (!(scale > 0.f) || !std::isfinite(scale)) return SPS_E_INVALID;
+  const sps_status s = sps::check_paged_rows(c, starts != nullptr, rows, max_tokens);
+  if (s != SPS_OK) return s;
+  const int qw = c.n_heads * c.head_dim;
+  if (!good_stride(q_stride, qw) || !good_stride(out_stride, qw)) return SPS_E_INVALID;
+  if (rows == 0) return SPS_OK;
+  if (!q || !out || q == out || !workspace || misaligned(q, c.dtype) || misaligned(out, c.dtype) ||
+      reinterpret_cast<uintptr_t>(workspace) % 256)
+    return SPS_E_INVALID;
+  const sps::PagedPlan p = sps::paged_plan(c, rows, max_tokens);
+  if (ws_bytes < p.total) return SPS_E_CAPACITY;
+  int* err = device_error_ptr();
+  if (!err) return SPS_E_HIP;
+  char* ws = static_cast<char*>(workspace);
+  SPS_HIP(sps::launch_paged_attention(c.dtype, paged_view(kv, layer), {starts, rows, max_tokens, pos_offset}, p, q,
+                                      q_stride, scale, window, out, out_stride, lse,
+                                      reinterpret_cast<float*>(ws + p.o_off), reinterpret_cast<float2*>(ws + p.ml_off),
+                                      err, as_stream(stream)));
   return SPS_OK;
 }
 

@@ -32,7 +32,8 @@ PURPOSE_DRAFT, PURPOSE_ACCEPT, PURPOSE_RESAMPLE = 0, 1, 2
 # grow with the rows and the cache capacity).
 PREFILL_ROWS = 160
 PREFILL_BYTES = 2 << 30
-DEV_BAD_TOKEN, DEV_EMPTY, DEV_CAPACITY, DEV_NONFINITE = 1, 2, 4, 8
+DEV_BAD_TOKEN, DEV_EMPTY, DEV_CAPACITY, DEV_NONFINITE, DEV_BAD_PAGE = 1, 2, 4, 8, 16
+ROPE_LAYOUT = {"half": 0, "interleaved": 1}
 
 
 class Config(ctypes.Structure):
@@ -58,6 +59,24 @@ def sampling_of(temperature, top_k=0, top_p=1.0):
 class AcceptIO(ctypes.Structure):
     _fields_ = [("p_draft", c_void_p), ("uniforms", c_void_p), ("rng", Philox),
                 ("out_tokens", c_void_p), ("n_accepted", c_void_p)]
+
+
+class RopeSpec(ctypes.Structure):
+    """Rotary pairs, frequencies and scaling (sps_rope_spec)."""
+    _fields_ = [("rot_dim", c_int32), ("layout", c_int32), ("base", c_float), ("factor", c_float),
+                ("original_len", c_int32), ("low_turns", c_float), ("high_turns", c_float), ("amplitude", c_float)]
+
+
+def rope_spec(rot_dim, base=10000.0, layout="half", factor=1.0, original_len=0, low_turns=1.0, high_turns=32.0,
+              amplitude=1.0):
+    return RopeSpec(int(rot_dim), ROPE_LAYOUT[layout], float(base), float(factor), int(original_len),
+                    float(low_turns), float(high_turns), float(amplitude))
+
+
+class PagedConfig(ctypes.Structure):
+    _fields_ = [("n_heads", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32), ("dtype", c_int32),
+                ("n_layers", c_int32), ("n_pages", c_int32), ("page_size", c_int32), ("B", c_int32),
+                ("max_pages", c_int32)]
 
 
 def _sig(name, res, args):
@@ -92,6 +111,17 @@ _sig("sps_commit", c_int32, [P, P, P, P, c_int32, c_int32, P, P, P, c_int32, P])
 _sig("sps_philox_uniforms", c_int32, [Philox, c_int32, c_int32, c_int32, P, P])
 _sig("sps_softmax", c_int32, [P, c_int32, c_int32, Sampling, P, P])
 _sig("sps_device_error", c_int32, [P, c_int32, ctypes.POINTER(c_int32)])
+c_int64 = ctypes.c_int64
+_sig("sps_rope", c_int32, [P, c_int64, P, ctypes.POINTER(RopeSpec), c_int32, c_int32, c_int32, c_int32, c_int32, P,
+                           c_int64, P])
+_sig("sps_paged_bytes", c_size_t, [ctypes.POINTER(PagedConfig)])
+_sig("sps_paged_create", c_int32, [ctypes.POINTER(PagedConfig), P, P, P, ctypes.POINTER(P)])
+_sig("sps_paged_destroy", None, [P])
+_sig("sps_paged_append", c_int32, [P, c_int32, P, c_int64, P, c_int64, ctypes.POINTER(RopeSpec), P, c_int64, P,
+                                   c_int64, P, c_int32, c_int32, c_int32, P])
+_sig("sps_paged_workspace_bytes", c_size_t, [ctypes.POINTER(PagedConfig), c_int32, c_int32])
+_sig("sps_paged_attention", c_int32, [P, c_int32, P, c_int64, P, c_int32, c_int32, c_int32, c_float, c_int32, P,
+                                      c_int64, P, P, c_size_t, P])
 _sig("sps_profile_gemm_begin", c_int32, [c_int32])
 _sig("sps_stream_read", c_int32, [P, c_size_t, P, P])
 _sig("sps_fp8_decode", c_int32, [P, c_int32, P, P])
@@ -105,7 +135,9 @@ EXPORTS = ["sps_status_string", "sps_abi_version", "sps_weight_bytes", "sps_pack
            "sps_kv_write", "sps_kv_read", "sps_workspace_bytes", "sps_forward", "sps_prefill_workspace_bytes", "sps_prefill", "sps_verify_step",
            "sps_accept_resample", "sps_draft_step", "sps_commit", "sps_philox_uniforms", "sps_softmax",
            "sps_device_error", "sps_profile_gemm_begin", "sps_profile_gemm_end",
-           "sps_stream_read", "sps_fp8_decode", "sps_weight_slot", "sps_verify_step_noalloc"]
+           "sps_stream_read", "sps_fp8_decode", "sps_weight_slot", "sps_verify_step_noalloc", "sps_rope",
+           "sps_paged_bytes", "sps_paged_create", "sps_paged_destroy", "sps_paged_append",
+           "sps_paged_workspace_bytes", "sps_paged_attention"]
 
 
 class SPSError(RuntimeError):
@@ -362,6 +394,159 @@ def fp8_decode(codes):
     out = torch.empty(codes.numel(), dtype=torch.float32, device=codes.device)
     check(lib.sps_fp8_decode(_ptr(codes, torch.uint8, "codes"), codes.numel(), _ptr(out), _stream()),
           "sps_fp8_decode")
+    return out
+
+
+def _raw_stream(dev):
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _here(t, dtype, name):
+    """The current device, on which the library runs its calls, if t is one of its tensors of `dtype`."""
+    if not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    dev = torch.cuda.current_device()
+    if t.get_device() != dev:
+        raise ValueError("%s is on device %d, the current device is %d" % (name, t.get_device(), dev))
+    if t.dtype != dtype:
+        raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    return dev
+
+
+def _heads(t, rows, heads, dim, dtype, name):
+    """(address, row stride) of a [rows][heads][dim] tensor whose rows may lie
+    apart (a slice of a wider one), each row's heads one after the other."""
+    _here(t, dtype, name)
+    if t.shape != (rows, heads, dim):
+        raise ValueError("%s must be [%d][%d][%d], got %s" % (name, rows, heads, dim, tuple(t.shape)))
+    s = t.stride()
+    if s[2] != 1 or (heads > 1 and s[1] != dim):
+        raise ValueError("%s: the heads of a row must lie one after the other" % name)
+    return t.data_ptr(), s[0] if rows > 1 else heads * dim
+
+
+def _flat(t, shape, dtype, name):
+    """Address of a contiguous tensor of that shape."""
+    _here(t, dtype, name)
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be contiguous %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    return t.data_ptr()
+
+
+def rope(x, positions, spec, out=None, backward=False):
+    """x [rows][heads][head_dim] (bf16 or fp32; rows may lie apart) rotated at
+    the int32 positions [rows], or with backward=True the gradient of that.
+    out may be x itself."""
+    if x.dim() != 3:
+        raise ValueError("x must be [rows][heads][head_dim], got %s" % (tuple(x.shape),))
+    if x.dtype != torch.float32 and x.dtype != torch.bfloat16:
+        raise ValueError("x must be float32 or bfloat16, got %s" % x.dtype)
+    rows, heads, dim = x.shape
+    dev = _here(x, x.dtype, "x")
+    if out is None:
+        out = torch.empty((rows, heads, dim), dtype=x.dtype, device=x.device)
+    xp, xs = _heads(x, rows, heads, dim, x.dtype, "x")
+    op, os_ = _heads(out, rows, heads, dim, x.dtype, "out")
+    check(lib.sps_rope(xp, xs, _flat(positions, (rows,), torch.int32, "positions"), ctypes.byref(spec), rows, heads,
+                       dim, 0 if x.dtype == torch.float32 else 1, 1 if backward else 0, op, os_, _raw_stream(dev)),
+          "sps_rope")
+    return out
+
+
+class PagedKV:
+    """A KV cache in pages: the buffer, the int32 page table [B][max_pages] and
+    committed lengths [B] (which the caller keeps up to date), and the handle.
+    `lengths` may be a KVCache's."""
+
+    def __init__(self, n_heads, n_kv_heads, head_dim, n_pages, page_size, B, max_pages, n_layers=1, dtype="bf16",
+                 buf=None, page_table=None, lengths=None, device="cuda"):
+        self.cfg = PagedConfig(n_heads, n_kv_heads, head_dim, DTYPE[dtype], n_layers, n_pages, page_size, B, max_pages)
+        self.n_heads, self.n_kv_heads, self.head_dim, self.B = n_heads, n_kv_heads, head_dim, B
+        self.n_layers, self.n_pages, self.page_size, self.max_pages = n_layers, n_pages, page_size, max_pages
+        nbytes = lib.sps_paged_bytes(ctypes.byref(self.cfg))
+        if nbytes == 0:
+            raise SPSError(2, "sps_paged_bytes")
+        self.dtype = TORCH_DTYPE[dtype]
+        shape = (n_layers, 2, n_pages, n_kv_heads, page_size * head_dim)
+        if buf is None:
+            buf = torch.empty(shape, dtype=self.dtype, device=device)
+        if page_table is None:
+            page_table = torch.full((B, max_pages), -1, dtype=torch.int32, device=device)
+        if lengths is None:
+            lengths = torch.zeros(B, dtype=torch.int32, device=device)
+        self.buf, self.page_table, self.lengths = buf, page_table, lengths
+        self.handle = c_void_p()
+        self._destroy = lib.sps_paged_destroy   # see Model.__init__
+        check(lib.sps_paged_create(ctypes.byref(self.cfg), _flat(buf, shape, self.dtype, "buf"),
+                                   _flat(page_table, (B, max_pages), torch.int32, "page_table"),
+                                   _flat(lengths, (B,), torch.int32, "lengths"), ctypes.byref(self.handle)),
+              "sps_paged_create")
+
+    def _rows(self, rows, starts, max_tokens):
+        if starts is None:
+            if max_tokens is None:
+                max_tokens = rows // self.B
+            return None, max_tokens
+        return _flat(starts, (self.B + 1,), torch.int32, "starts"), rows if max_tokens is None else max_tokens
+
+    def append(self, layer, k, v, rope=None, q=None, q_out=None, starts=None, max_tokens=None, pos_offset=0):
+        """Write the new tokens' k and v [rows][n_kv_heads][head_dim] into their
+        pages, k rotated by `rope` (a rope_spec; None: as it is), and with q
+        [rows][n_heads][head_dim] return the queries rotated alike (in q_out,
+        which may be q). Sequence b has rows starts[b] .. starts[b + 1] - 1, or
+        rows / B each; at most max_tokens (default: rows)."""
+        H, D, dt = self.n_kv_heads, self.head_dim, self.dtype
+        rows = k.shape[0]
+        dev = _here(self.buf, dt, "the cache")
+        kp, ks = _heads(k, rows, H, D, dt, "k")
+        vp, vs = _heads(v, rows, H, D, dt, "v")
+        qp = qop = None
+        qs = qos = 0
+        if q is not None:
+            qp, qs = _heads(q, rows, self.n_heads, D, dt, "q")
+            if q_out is None:
+                q_out = torch.empty((rows, self.n_heads, D), dtype=dt, device=q.device)
+            qop, qos = _heads(q_out, rows, self.n_heads, D, dt, "q_out")
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        sp, most = self._rows(rows, starts, max_tokens)
+        check(lib.sps_paged_append(self.handle, layer, kp, ks, vp, vs, None if rope is None else ctypes.byref(rope), qp,
+                                   qs, qop, qos, sp, rows, most, pos_offset, _raw_stream(dev)), "sps_paged_append")
+        return q_out
+
+    def workspace(self, rows, max_tokens):
+        """Scratch for paged_attention of up to `rows` rows, at most max_tokens of one sequence."""
+        n = lib.sps_paged_workspace_bytes(ctypes.byref(self.cfg), rows, max_tokens)
+        if n == 0:
+            raise SPSError(2, "sps_paged_workspace_bytes")
+        return torch.empty(n, dtype=torch.uint8, device=self.buf.device)
+
+    def __del__(self):
+        h, destroy = getattr(self, "handle", None), getattr(self, "_destroy", None)
+        if h is not None and h.value and destroy is not None:
+            destroy(h)
+        self.handle = None
+
+
+def paged_attention(kv, layer, q, ws, out=None, lse=None, starts=None, max_tokens=None, pos_offset=0, scale=None,
+                    window=0):
+    """Attention of the new tokens' q [rows][n_heads][head_dim] over the pages
+    of their sequences (their own keys and values appended before), each row
+    over the positions up to its own, at most `window` of them (0: all). lse:
+    fp32 [rows][n_heads] for the log of every row's sum. Rows as for append;
+    scale defaults to head_dim ** -0.5."""
+    rows, H, D = q.shape[0], kv.n_heads, kv.head_dim
+    dev = _here(kv.buf, kv.dtype, "the cache")
+    qp, qs = _heads(q, rows, H, D, kv.dtype, "q")
+    if out is None:
+        out = torch.empty((rows, H, D), dtype=kv.dtype, device=q.device)
+    op, os_ = _heads(out, rows, H, D, kv.dtype, "out")
+    lp = None if lse is None else _flat(lse, (rows, H), torch.float32, "lse")
+    sp, most = kv._rows(rows, starts, max_tokens)
+    _here(ws, torch.uint8, "the workspace")
+    check(lib.sps_paged_attention(kv.handle, layer, qp, qs, sp, rows, most, pos_offset,
+                                  D ** -0.5 if scale is None else scale, window, op, os_, lp, ws.data_ptr(),
+                                  ws.numel(), _raw_stream(dev)), "sps_paged_attention")
     return out
 
 
