@@ -87,62 +87,63 @@ __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_ex
 // Scores of one block for one query tile with the positions a row does not see
 // at -Inf. vis collects, per lane, which of its eight positions its row sees.
 template <typename T, int DH>
-__device__ __forceinline__ void block_scores(const Frag<T> (&kf)[2][DH / 32], const Frag<T> (&qf)[DH / 32], int pos0,
-                                             int qpos, int window, int end, bool masked, int grp, f32x4 (&s)[2],
-                                             uint32_t* vis) {
+__device__ __forceinline__ void block_scores(const Frag<T> (&kf)[2][DH / 32], const Frag<T> (&qf)[DH / 32],
+                                             f32x4 (&s)[2]) {
 #pragma unroll
   for (int pt = 0; pt < 2; ++pt) {
     s[pt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int dt = 0; dt < DH / 32; ++dt) s[pt] = mma8(s[pt], kf[pt][dt], qf[dt]);
   }
-  *vis = 0xff;
-  if (masked) {
-    *vis = 0;
-    const int lo = window ? qpos - window : -1;
-#pragma unroll
-    for (int pt = 0; pt < 2; ++pt)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int pos = pos0 + pt * 16 + grp * 4 + r;
-        const bool seen = pos <= qpos && pos > lo && pos < end;
-        s[pt][r] = seen ? s[pt][r] : -INFINITY;
-        *vis |= seen ? 1u << (pt * 4 + r) : 0;
-      }
-  }
 }
-
-// Online softmax step on one tile's scores: the weights as a hi + lo pair of
-// bf16 values (p = hi + lo to 2^-16 relative; the second product costs nothing
-// where the loads of K and V are what takes the time), or fp32.
-template <typename T, int DH>
-__device__ __forceinline__ void softmax_step(const f32x4 (&s)[2], float c_log2, float& m_run, float& l_run,
-                                             f32x4 (&o)[DH / 16], Frag<T>& hi, Frag<T>& lo) {
-  float mx = -INFINITY;
+__device__ __forceinline__ uint32_t mask_scores(int pos0, int qpos, int window, int end, int grp, f32x4 (&s)[2]) {
+  uint32_t vis = 0;
+  const int lo = window ? qpos - window : -1;
 #pragma unroll
   for (int pt = 0; pt < 2; ++pt)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[pt][r]);
-  mx = fmaxf(mx, __shfl_xor(mx, 16));
-  mx = fmaxf(mx, __shfl_xor(mx, 32));
-  const float m_new = fmaxf(m_run, mx);
-  const float m_use = m_new == -INFINITY ? 0.f : m_new;
-  const float alpha = fast_exp2((m_run - m_use) * c_log2);
+    for (int r = 0; r < 4; ++r) {
+      const int pos = pos0 + pt * 16 + grp * 4 + r;
+      const bool seen = pos <= qpos && pos > lo && pos < end;
+      s[pt][r] = seen ? s[pt][r] : -INFINITY;
+      vis |= seen ? 1u << (pt * 4 + r) : 0;
+    }
+  return vis;
+}
+
+// Online softmax step on one tile's scores. The reference that is taken off
+// the scaled scores (ref, in units of log2) follows the running maximum only
+// once that is kLag above it: weights are at most 2^kLag instead of 1, which
+// fp32 sums and bf16 weights hold as precisely, and the accumulators are
+// rescaled a few times per row instead of in nearly every block. Each lane
+// sums its own positions' weights.
+constexpr float kLag = 8.f;
+template <typename T, int DH>
+__device__ __forceinline__ void softmax_step(f32x4 (&s)[2], float c_log2, float& ref, float& l_run,
+                                             f32x4 (&o)[DH / 16]) {
+  float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                   fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) * c_log2;
+  if (__ballot(mx > ref + kLag)) {
+    mx = fmaxf(mx, __shfl_xor(mx, 16));
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    if (mx > ref + kLag) {                         // alike in the four lanes of a row
+      const float alpha = fast_exp2(ref - mx);     // 0 for the row's first reference
+      ref = mx;
+      l_run *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DH / 16; ++dt) o[dt] *= alpha;
+    }
+  }
+  const float off = ref == -INFINITY ? 0.f : ref;
   float ps = 0.f;
 #pragma unroll
   for (int pt = 0; pt < 2; ++pt)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const float pv = fast_exp2((s[pt][r] - m_use) * c_log2);
-      const T h = from_f32<T>(pv);
-      hi.v[pt * 4 + r] = h;
-      lo.v[pt * 4 + r] = from_f32<T>(pv - to_f32(h));
-      ps += pv;
+      s[pt][r] = fast_exp2(fmaf(s[pt][r], c_log2, -off));
+      ps += s[pt][r];
     }
-  l_run = l_run * alpha + ps;
-  m_run = m_new;
-#pragma unroll
-  for (int dt = 0; dt < DH / 16; ++dt) o[dt] *= alpha;
+  l_run += ps;
 }
 
 // Values that are not finite, in a block with positions that not every row of
@@ -182,8 +183,12 @@ __device__ __forceinline__ void infinite_values(Frag<T> (&vf)[DH / 16], const ui
       if (nonfinite(vf[dt].v[e])) vf[dt].v[e] = from_f32<T>(0.f);
 }
 
+constexpr int decode_waves(int es, int DH, int QT) {
+  const int regs = DH * es / 4 + DH * QT * 3 / 8 * (es == 4 ? 4 : 3) / 3 + 90;
+  return regs <= 168 ? 3 : regs <= 256 ? 2 : 1;
+}
 template <typename T, int DH, int QT>
-__global__ __launch_bounds__(256) void paged_attn_kernel(PagedView c, PagedRows r, int target,
+__global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_attn_kernel(PagedView c, PagedRows r, int target,
                                                          const T* __restrict__ q, int64_t ldq, float scale, int window,
                                                          T* __restrict__ out, int64_t ldo, float* __restrict__ lse,
                                                          float* __restrict__ part_o, float2* __restrict__ part_ml,
@@ -223,22 +228,28 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedView c, PagedRows 
     for (int dt = 0; dt < DH / 32; ++dt)
       qf[qt][dt] = valid ? load_frag_any(q + tok[qt] * ldq + head[qt] * DH + dt * 32 + grp * 8) : Frag<T>::zero();
   }
-  float m_run[QT], l_run[QT];
+  float ref[QT], l_run[QT];
   f32x4 o[QT][ND];
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {
-    m_run[qt] = -INFINITY;
+    ref[qt] = -INFINITY;
     l_run[qt] = 0.f;
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // This wave's blocks are blk0 + wave + 4 i; the pages of 64 of them at a time.
+  // This wave's blocks are blk0 + wave + 4 i; the pages of 64 of them at a
+  // time. The next block's keys are asked for once the scores are done with
+  // this one's, its values once the products are: one block's registers keep
+  // the loads going.
   const int32_t* tab = c.table + static_cast<size_t>(pl.b) * c.max_pages;
   const size_t area = static_cast<size_t>(DH) << c.page_log2;
+  const int in_page = (1 << c.page_log2) - 1;
   const int nb = blk1 > blk0 + wave ? (blk1 - blk0 - wave + 3) / 4 : 0;
-  for (int i0 = 0; i0 < nb; i0 += 64) {
-    int id = -1;
+  int id = -1, id0 = 0;                            // the pages of blocks id0 .. id0 + 63, one a lane
+  auto pages = [&](int i0) {
+    id0 = i0;
+    id = -1;
     if (i0 + lane < nb) {
       id = tab[(blk0 + wave + 4 * (i0 + lane)) >> (c.page_log2 - 5)];
       if (id < 0 || id >= c.n_pages) {
@@ -246,57 +257,87 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedView c, PagedRows 
         id = -1;
       }
     }
-    const int n = min(64, nb - i0);
-    for (int i = 0; i < n; ++i) {
-      const int page = __builtin_amdgcn_readlane(id, i);
+  };
+  // The first block from i on whose page is good (nb: none), and its place.
+  size_t off = 0;
+  auto seek = [&](int i) {
+    for (; i < nb; ++i) {
+      if (i - id0 >= 64) pages(i);
+      const int page = __builtin_amdgcn_readlane(id, i - id0);
       if (page < 0) continue;
-      const int blk = blk0 + wave + 4 * (i0 + i), pos0 = blk * 32;
-      const size_t off = (static_cast<size_t>(page) * c.H + pl.kvh) * area +
-                         static_cast<size_t>(pos0 & ((1 << c.page_log2) - 1)) * DH + lane * 8;
-      const T* kp = static_cast<const T*>(c.k) + off;
-      const T* vp = static_cast<const T*>(c.v) + off;
-      Frag<T> kf[2][DH / 32], vf[ND];
-#pragma unroll
-      for (int pt = 0; pt < 2; ++pt)
-#pragma unroll
-        for (int dt = 0; dt < DH / 32; ++dt) kf[pt][dt] = load_frag(kp + (pt * (DH / 32) + dt) * 512);
-#pragma unroll
-      for (int dt = 0; dt < ND; ++dt) vf[dt] = load_frag(vp + dt * 512);
-      const bool masked = pos0 + 31 > first || pos0 + 31 >= end || (window && pos0 <= last - window);
-      if (pos0 + 32 > end) {
-        // Positions no row of the tile sees hold anything, and 0 x NaN is not 0.
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (pos0 + (e < 4 ? grp * 4 + e : 16 + grp * 4 + e - 4) >= end) {
-#pragma unroll
-            for (int dt = 0; dt < ND; ++dt) vf[dt].v[e] = from_f32<T>(0.f);
-          }
-      }
-      f32x4 sc[QT][2];
-      uint32_t vis[QT];
-#pragma unroll
-      for (int qt = 0; qt < QT; ++qt)
-        block_scores<T, DH>(kf, qf[qt], pos0, qpos[qt], window, end, masked, grp, sc[qt], &vis[qt]);
-      Frag<T> hi[QT], lw[QT];
-#pragma unroll
-      for (int qt = 0; qt < QT; ++qt)
-        softmax_step<T, DH>(sc[qt], c_log2, m_run[qt], l_run[qt], o[qt], hi[qt], lw[qt]);
-      if (masked) {
-        bool odd = false;
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) odd |= nonfinite(vf[dt].v[e]);
-        if (__ballot(odd)) infinite_values<T, DH, QT>(vf, vis, o);
-      }
-#pragma unroll
-      for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-        for (int qt = 0; qt < QT; ++qt) {
-          o[qt][dt] = mma8(o[qt][dt], vf[dt], hi[qt]);
-          if (sizeof(T) == 2) o[qt][dt] = mma8(o[qt][dt], vf[dt], lw[qt]);
-        }
+      off = (static_cast<size_t>(page) * c.H + pl.kvh) * area +
+            static_cast<size_t>((blk0 + wave + 4 * i) * 32 & in_page) * DH + lane * 8;
+      break;
     }
+    return i;
+  };
+  Frag<T> kf[2][DH / 32], vf[ND];
+  auto load_keys = [&] {
+    const T* kp = static_cast<const T*>(c.k) + off;
+#pragma unroll
+    for (int pt = 0; pt < 2; ++pt)
+#pragma unroll
+      for (int dt = 0; dt < DH / 32; ++dt) kf[pt][dt] = load_frag_stream(kp + (pt * (DH / 32) + dt) * 512);
+  };
+  auto load_values = [&] {
+    const T* vp = static_cast<const T*>(c.v) + off;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) vf[dt] = load_frag_stream(vp + dt * 512);
+  };
+  pages(0);
+  int i = seek(0);
+  if (i < nb) {
+    load_keys();
+    load_values();
+  }
+  while (i < nb) {
+    const int pos0 = (blk0 + wave + 4 * i) * 32;
+    f32x4 sc[QT][2];
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) block_scores<T, DH>(kf, qf[qt], sc[qt]);
+    const int next = seek(i + 1);
+    if (next < nb) load_keys();
+    const bool masked = pos0 + 31 > first || pos0 + 31 >= end || (window && pos0 <= last - window);
+    uint32_t vis[QT];
+    if (masked) {
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) vis[qt] = mask_scores(pos0, qpos[qt], window, end, grp, sc[qt]);
+    }
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) softmax_step<T, DH>(sc[qt], c_log2, ref[qt], l_run[qt], o[qt]);
+    if (masked) {
+      // Positions no row of the tile sees hold anything, and 0 x NaN is not 0.
+      bool odd = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const bool past = pos0 + (e < 4 ? grp * 4 + e : 16 + grp * 4 + e - 4) >= end;
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) {
+          if (past) vf[dt].v[e] = from_f32<T>(0.f);
+          odd |= nonfinite(vf[dt].v[e]);
+        }
+      }
+      if (__ballot(odd)) infinite_values<T, DH, QT>(vf, vis, o);
+    }
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      // bf16: the weights as hi + lo, p to 2^-16 relative; the second product
+      // costs nothing where the loads are what takes the time.
+      Frag<T> hi, lw;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float p = sc[qt][e >> 2][e & 3];
+        hi.v[e] = from_f32<T>(p);
+        lw.v[e] = from_f32<T>(p - to_f32(hi.v[e]));
+      }
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) {
+        o[qt][dt] = mma8(o[qt][dt], vf[dt], hi);
+        if (sizeof(T) == 2) o[qt][dt] = mma8(o[qt][dt], vf[dt], lw);
+      }
+    }
+    if (next < nb) load_values();
+    i = next;
   }
 
   // Waves 2, 3 into 0, 1, then 1 into 0.
@@ -311,7 +352,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedView c, PagedRows 
     if (wave >= half && wave < 2 * half) {
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
-        sml[((wave - half) * QT + qt) * 64 + lane] = make_float2(m_run[qt], l_run[qt]);
+        sml[((wave - half) * QT + qt) * 64 + lane] = make_float2(ref[qt], l_run[qt]);
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) sm[(((wave - half) * QT + qt) * ND + dt) * 64 + lane] = o[qt][dt];
       }
@@ -321,9 +362,9 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedView c, PagedRows 
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
         const float2 ml = sml[(wave * QT + qt) * 64 + lane];
-        const float m = fmaxf(m_run[qt], ml.x), mu = m == -INFINITY ? 0.f : m;
-        const float a = fast_exp2((m_run[qt] - mu) * c_log2), b = fast_exp2((ml.x - mu) * c_log2);
-        m_run[qt] = m;
+        const float m = fmaxf(ref[qt], ml.x), mu = m == -INFINITY ? 0.f : m;
+        const float a = fast_exp2(ref[qt] - mu), b = fast_exp2(ml.x - mu);
+        ref[qt] = m;
         l_run[qt] = a * l_run[qt] + b * ml.y;
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) o[qt][dt] = a * o[qt][dt] + b * sm[((wave * QT + qt) * ND + dt) * 64 + lane];
@@ -338,7 +379,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedView c, PagedRows 
     if (row >= nrows) continue;
     if (pl.ranges > 1) {
       const size_t at = (pl.slot + static_cast<long>(pl.range) * c.H) * TR + qt * 16 + r16;
-      if (grp == 0) part_ml[at] = make_float2(m_run[qt], l_run[qt]);
+      if (grp == 0) part_ml[at] = make_float2(ref[qt], l_run[qt]);
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt)
         *reinterpret_cast<f32x4*>(part_o + at * DH + dt * 16 + grp * 4) = o[qt][dt];
@@ -350,7 +391,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedView c, PagedRows 
       for (int dt = 0; dt < ND; ++dt) store4_any(dst + dt * 16, l_run[qt] == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[qt][dt] * inv);
       if (lse && grp == 0)
         lse[static_cast<size_t>(tok[qt]) * c.H * c.G + head[qt]] =
-            l_run[qt] == 0.f ? -INFINITY : m_run[qt] * scale + logf(l_run[qt]);
+            l_run[qt] == 0.f ? -INFINITY : 0.69314718f * ref[qt] + logf(l_run[qt]);
     }
   }
 }
@@ -358,7 +399,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedView c, PagedRows 
 // The ranges of a tile's rows joined: one wave per row.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedView c, PagedRows r, int target, int tile_rows,
-                                                         float scale, int window, const float* __restrict__ part_o,
+                                                         int window, const float* __restrict__ part_o,
                                                          const float2* __restrict__ part_ml, T* __restrict__ out,
                                                          int64_t ldo, float* __restrict__ lse) {
   __shared__ int words[2 * kMaxPagedB];
@@ -368,7 +409,6 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedView c, PagedRows 
   const int lane = threadIdx.x & 63, in = blockIdx.y * 4 + (threadIdx.x >> 6);
   const int row = pl.tile * tile_rows + in;
   if (row >= s.n * c.G) return;
-  const float c_log2 = scale * 1.4426950408889634f;
   const float2* ml = part_ml + pl.slot * tile_rows + in;
   const float* po = part_o + (pl.slot * tile_rows + in) * DH + lane * (DH / 64);
   const size_t step = static_cast<size_t>(c.H) * tile_rows;      // from range to range
@@ -381,7 +421,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedView c, PagedRows 
     for (int i = 0; i < pl.ranges; ++i) {
       const float2 x = ml[i * step];
       if (x.x == -INFINITY) continue;
-      const float w = fast_exp2((x.x - m) * c_log2);
+      const float w = fast_exp2(x.x - m);
       l += w * x.y;
 #pragma unroll
       for (int d = 0; d < DH / 64; ++d) acc[d] += w * po[i * step * DH + d];
@@ -392,20 +432,23 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedView c, PagedRows 
   for (int d = 0; d < DH / 64; ++d)
     out[tok * ldo + head * DH + lane * (DH / 64) + d] = from_f32<T>(l == 0.f ? 0.f : acc[d] / l);
   if (lse && lane == 0)
-    lse[static_cast<size_t>(tok) * c.H * c.G + head] = l == 0.f ? -INFINITY : m * scale + logf(l);
+    lse[static_cast<size_t>(tok) * c.H * c.G + head] = l == 0.f ? -INFINITY : 0.69314718f * m + logf(l);
 }
 
 template <typename T, int DH>
 static hipError_t attn_t(const PagedView& c, const PagedRows& r, const PagedPlan& p, const void* q, int64_t ldq,
                          float scale, int window, void* out, int64_t ldo, float* lse, float* part_o, float2* part_ml,
                          int* err, hipStream_t st) {
-  auto kern = p.qt == 1 ? paged_attn_kernel<T, DH, 1> : paged_attn_kernel<T, DH, 2>;
+  auto kern = p.qt == 1   ? paged_attn_kernel<T, DH, 1>
+              : p.qt == 2 ? paged_attn_kernel<T, DH, 2>
+              : p.qt == 3 ? paged_attn_kernel<T, DH, 3>
+                          : paged_attn_kernel<T, DH, 4>;
   hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(p.items)), dim3(256), 0, st, c, r, p.target,
                      static_cast<const T*>(q), ldq, scale, window, static_cast<T*>(out), ldo, lse, part_o, part_ml, err);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.joins == 0) return e;
   hipLaunchKernelGGL((paged_join_kernel<T, DH>), dim3(static_cast<unsigned>(p.joins), 4 * p.qt), dim3(256), 0, st, c, r,
-                     p.target, 16 * p.qt, scale, window, part_o, part_ml, static_cast<T*>(out), ldo, lse);
+                     p.target, 16 * p.qt, window, part_o, part_ml, static_cast<T*>(out), ldo, lse);
   return hipGetLastError();
 }
 

@@ -285,7 +285,7 @@ PagedPlan paged_plan(const sps_paged_config& c, int rows, int max_tokens) {
   PagedPlan p{};
   const int G = c.n_heads / c.n_kv_heads;
   const long q = static_cast<long>(std::min(rows, max_tokens)) * G;
-  p.qt = q <= 16 ? 1 : 2;
+  p.qt = q <= 48 ? static_cast<int>((q + 15) / 16) : 4;
   p.target = 4 * kCUs;
   const long tile = 16L * p.qt;
   // Every sequence's last tile may be partly filled.
@@ -313,7 +313,7 @@ size_t paged_workspace_bytes(const sps_paged_config* c, int rows, int max_tokens
   // Calls with fewer tokens per sequence have smaller tiles and may have more of them.
   size_t most = 256;
   const int G = c->n_heads / c->n_kv_heads;
-  for (long q : {16L, static_cast<long>(kMaxPagedRows)})
+  for (long q : {16L, 32L, 48L, static_cast<long>(kMaxPagedRows)})
     most = std::max(most, paged_plan(*c, rows, static_cast<int>(std::max(1L, std::min<long>(max_tokens, q / G)))).total);
   return most;
 }
