@@ -109,7 +109,7 @@ hipError_t launch_paged_append(int dtype, const PagedView& c, const PagedRows& r
                                int64_t ldqo, int* err, hipStream_t st);
 hipError_t launch_paged_attention(int dtype, const PagedView& c, const PagedRows& r, const PagedPlan& p, const void* q,
                                   int64_t ldq, float scale, int window, void* out, int64_t ldo, float* lse,
-                                  float* part_o, float2* part_ml, int* err, hipStream_t st);
+                                  char* workspace, int* err, hipStream_t st);
 
 // Sampling.
 // Row statistics (stats, row_stat_bytes() each, may be NULL) and, if probs

@@ -19,13 +19,18 @@ struct Place {
   long slot;               // of the tile's first range (ranges > 1)
 };
 
-// The tiles and blocks of every sequence of the call, per sequence in LDS,
+// Sequences with more than `above` and up to `limit` query rows, in tiles of
+// `tile` (plan.h).
+struct Class {
+  int tile, target, above, limit;
+};
+
+// The tiles and blocks of every sequence of the class, per sequence in LDS,
 // and from them the place of item (join: of the (tile, KV head) pair) number
 // `idx`. Every work-group of both launches computes the same plan from the
 // same lengths. Returns false past the last one.
-__device__ __forceinline__ bool find_place(const PagedView& c, const PagedRows& r, int window, int tile_rows,
-                                           int target, bool join, long idx, int* s_tiles, int* s_blocks, int* err,
-                                           Place* out) {
+__device__ __forceinline__ bool find_place(const PagedView& c, const PagedRows& r, int window, const Class& k,
+                                           bool join, long idx, int* s_tiles, int* s_blocks, int* err, Place* out) {
   const int lane = threadIdx.x & 63;
   const int cap = c.max_pages << c.page_log2;
   for (int b = threadIdx.x; b < c.B; b += blockDim.x) {
@@ -33,14 +38,15 @@ __device__ __forceinline__ bool find_place(const PagedView& c, const PagedRows& 
     if (s.bad && idx == 0 && err) atomicOr(err, kErrCapacity);
     const int end = min(max(s.p0 + s.n, 0), cap);
     const int lo = window ? min(max(s.p0 - window + 1, 0), end) : 0;
-    s_tiles[b] = (s.n * c.G + tile_rows - 1) / tile_rows;
+    const int rows = s.n * c.G;
+    s_tiles[b] = rows > k.above && rows <= k.limit ? (rows + k.tile - 1) / k.tile : 0;
     s_blocks[b] = (end + 31) / 32 - lo / 32;
   }
   __syncthreads();
   uint64_t all = 0;
   for (int b0 = 0; b0 < c.B; b0 += 64)
     all += wave_sum_u64(b0 + lane < c.B ? static_cast<uint64_t>(s_tiles[b0 + lane]) * s_blocks[b0 + lane] : 0);
-  const int per = max(kPagedMinBlocks, static_cast<int>(ceil(static_cast<double>(all) * c.H / target)));
+  const int per = max(kPagedMinBlocks, static_cast<int>(ceil(static_cast<double>(all) * c.H / k.target)));
   const int h = static_cast<int>(idx % c.H);
   const uint32_t want = static_cast<uint32_t>(idx / c.H);
   uint64_t before = 0;                             // (items or joins) << 32 | slots, per KV head
@@ -84,31 +90,14 @@ template <> __device__ __forceinline__ bool nonfinite<float>(float x) {
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Scores of one block for one query tile with the positions a row does not see
-// at -Inf. vis collects, per lane, which of its eight positions its row sees.
-template <typename T, int DH>
-__device__ __forceinline__ void block_scores(const Frag<T> (&kf)[2][DH / 32], const Frag<T> (&qf)[DH / 32],
-                                             f32x4 (&s)[2]) {
-#pragma unroll
-  for (int pt = 0; pt < 2; ++pt) {
-    s[pt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int dt = 0; dt < DH / 32; ++dt) s[pt] = mma8(s[pt], kf[pt][dt], qf[dt]);
-  }
-}
-__device__ __forceinline__ uint32_t mask_scores(int pos0, int qpos, int window, int end, int grp, f32x4 (&s)[2]) {
-  uint32_t vis = 0;
+// Scores (of 16 positions from pos0 on) at positions that a row does not see go to -Inf.
+__device__ __forceinline__ void mask_scores(int pos0, int qpos, int window, int end, int grp, f32x4& s) {
   const int lo = window ? qpos - window : -1;
 #pragma unroll
-  for (int pt = 0; pt < 2; ++pt)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int pos = pos0 + pt * 16 + grp * 4 + r;
-      const bool seen = pos <= qpos && pos > lo && pos < end;
-      s[pt][r] = seen ? s[pt][r] : -INFINITY;
-      vis |= seen ? 1u << (pt * 4 + r) : 0;
-    }
-  return vis;
+  for (int r = 0; r < 4; ++r) {
+    const int pos = pos0 + grp * 4 + r;
+    s[r] = pos <= qpos && pos > lo && pos < end ? s[r] : -INFINITY;
+  }
 }
 
 // Online softmax step on one tile's scores. The reference that is taken off
@@ -118,11 +107,12 @@ __device__ __forceinline__ uint32_t mask_scores(int pos0, int qpos, int window, 
 // rescaled a few times per row instead of in nearly every block. Each lane
 // sums its own positions' weights.
 constexpr float kLag = 8.f;
-template <typename T, int DH>
-__device__ __forceinline__ void softmax_step(f32x4 (&s)[2], float c_log2, float& ref, float& l_run,
-                                             f32x4 (&o)[DH / 16]) {
-  float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
-                   fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) * c_log2;
+template <int NP, int ND>
+__device__ __forceinline__ void softmax_step(f32x4 (&s)[NP], float c_log2, float& ref, float& l_run, f32x4 (&o)[ND]) {
+  float mx = -INFINITY;
+#pragma unroll
+  for (int pt = 0; pt < NP; ++pt) mx = fmaxf(mx, fmaxf(fmaxf(s[pt][0], s[pt][1]), fmaxf(s[pt][2], s[pt][3])));
+  mx *= c_log2;
   if (__ballot(mx > ref + kLag)) {
     mx = fmaxf(mx, __shfl_xor(mx, 16));
     mx = fmaxf(mx, __shfl_xor(mx, 32));
@@ -131,13 +121,13 @@ __device__ __forceinline__ void softmax_step(f32x4 (&s)[2], float c_log2, float&
       ref = mx;
       l_run *= alpha;
 #pragma unroll
-      for (int dt = 0; dt < DH / 16; ++dt) o[dt] *= alpha;
+      for (int dt = 0; dt < ND; ++dt) o[dt] *= alpha;
     }
   }
   const float off = ref == -INFINITY ? 0.f : ref;
   float ps = 0.f;
 #pragma unroll
-  for (int pt = 0; pt < 2; ++pt)
+  for (int pt = 0; pt < NP; ++pt)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       s[pt][r] = fast_exp2(fmaf(s[pt][r], c_log2, -off));
@@ -146,41 +136,70 @@ __device__ __forceinline__ void softmax_step(f32x4 (&s)[2], float c_log2, float&
   l_run += ps;
 }
 
-// Values that are not finite, in a block with positions that not every row of
-// the tile sees: 0 x Inf would carry them into rows that do not see them. They
-// are taken out of the tile, and put into the rows that do see them by
-// counting, per row and dim, visible +Inf, -Inf and NaN with products of ones.
-template <typename T, int DH, int QT>
-__device__ __forceinline__ void infinite_values(Frag<T> (&vf)[DH / 16], const uint32_t (&vis)[QT], f32x4 (&o)[QT][DH / 16]) {
-  float inf = INFINITY;
+// Values of a block in which some row of the tile does not see some position:
+// 0 x Inf would carry a value that is not finite into the rows that do not see
+// it. Positions past the last one (they may hold anything) are cleared; other
+// values that are not finite are taken out of the fragment too, and put into
+// the rows that see them by counting, per row and dim, visible +Inf, -Inf and
+// NaN with products of ones.
+template <typename T, int QT, int ND>
+__device__ __forceinline__ void clean_values(Frag<T>& vf, int pos0, const int (&qpos)[QT], int window, int end, int grp,
+                                             f32x4 (&o)[QT][ND], int dt) {
+  bool odd = false;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (pos0 + (e >> 2) * 16 + grp * 4 + (e & 3) >= end) vf.v[e] = from_f32<T>(0.f);
+    odd |= nonfinite(vf.v[e]);
+  }
+  if (!__ballot(odd)) return;
 #pragma unroll 1
   for (int kind = 0; kind < 3; ++kind) {
+    const float what = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+    Frag<T> one;
 #pragma unroll
-    for (int dt = 0; dt < DH / 16; ++dt) {
-      Frag<T> one;
+    for (int e = 0; e < 8; ++e) {
+      const float x = to_f32(vf.v[e]);
+      one.v[e] = from_f32<T>((kind == 2 ? x != x : x == what) ? 1.f : 0.f);
+    }
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      Frag<T> see;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float x = to_f32(vf[dt].v[e]);
-        const bool is = kind == 0 ? x == INFINITY : kind == 1 ? x == -INFINITY : x != x;
-        one.v[e] = from_f32<T>(is ? 1.f : 0.f);
+        const int pos = pos0 + (e >> 2) * 16 + grp * 4 + (e & 3);
+        see.v[e] = from_f32<T>(pos <= qpos[qt] && (!window || pos > qpos[qt] - window) && pos < end ? 1.f : 0.f);
       }
+      const f32x4 n = mma8(f32x4{0.f, 0.f, 0.f, 0.f}, one, see);
 #pragma unroll
-      for (int qt = 0; qt < QT; ++qt) {
-        Frag<T> see;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) see.v[e] = from_f32<T>(vis[qt] >> e & 1 ? 1.f : 0.f);
-        const f32x4 n = mma8(f32x4{0.f, 0.f, 0.f, 0.f}, one, see);
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (n[r] > 0.f) o[qt][dt][r] += kind == 0 ? inf : kind == 1 ? -inf : NAN;
-      }
+      for (int r = 0; r < 4; ++r)
+        if (n[r] > 0.f) o[qt][dt][r] += what;
     }
   }
 #pragma unroll
-  for (int dt = 0; dt < DH / 16; ++dt)
+  for (int e = 0; e < 8; ++e)
+    if (nonfinite(vf.v[e])) vf.v[e] = from_f32<T>(0.f);
+}
+
+// Row `in` of a tile (its dims 16 dt + 4 grp .. + 3 in this lane): the output,
+// or a partial if the tile has more ranges.
+template <typename T, int DH>
+__device__ __forceinline__ void write_row(const PagedView& c, const Class& k, const Place& pl, int in, int tok, int head,
+                                          int grp, float ref, float l, const f32x4 (&o)[DH / 16], T* out, int64_t ldo,
+                                          float* lse, float* part_o, float2* part_ml) {
+  if (pl.ranges > 1) {
+    const size_t at = (pl.slot + static_cast<long>(pl.range) * c.H) * k.tile + in;
+    if (grp == 0) part_ml[at] = make_float2(ref, l);
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (nonfinite(vf[dt].v[e])) vf[dt].v[e] = from_f32<T>(0.f);
+    for (int dt = 0; dt < DH / 16; ++dt) *reinterpret_cast<f32x4*>(part_o + at * DH + dt * 16 + grp * 4) = o[dt];
+    return;
+  }
+  // A sum of zero: no visible position, or none with weight.
+  const float inv = 1.f / l;
+  T* dst = out + tok * ldo + head * DH + grp * 4;
+#pragma unroll
+  for (int dt = 0; dt < DH / 16; ++dt) store4_any(dst + dt * 16, l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[dt] * inv);
+  if (lse && grp == 0)
+    lse[static_cast<size_t>(tok) * c.H * c.G + head] = l == 0.f ? -INFINITY : 0.69314718f * ref + logf(l);
 }
 
 constexpr int decode_waves(int es, int DH, int QT) {
@@ -188,7 +207,7 @@ constexpr int decode_waves(int es, int DH, int QT) {
   return regs <= 168 ? 3 : regs <= 256 ? 2 : 1;
 }
 template <typename T, int DH, int QT>
-__global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_attn_kernel(PagedView c, PagedRows r, int target,
+__global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_few_kernel(PagedView c, PagedRows r, Class k,
                                                          const T* __restrict__ q, int64_t ldq, float scale, int window,
                                                          T* __restrict__ out, int64_t ldo, float* __restrict__ lse,
                                                          float* __restrict__ part_o, float2* __restrict__ part_ml,
@@ -200,7 +219,7 @@ __global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_at
   __shared__ float2 sml[2 * QT * 64];
   int* s_tiles = reinterpret_cast<int*>(sm);
   Place pl;
-  if (!find_place(c, r, window, TR, target, false, blockIdx.x, s_tiles, s_tiles + kMaxPagedB, err, &pl)) return;
+  if (!find_place(c, r, window, k, false, blockIdx.x, s_tiles, s_tiles + kMaxPagedB, err, &pl)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int r16 = lane & 15, grp = lane >> 4;
   const SeqRows s = seq_rows(c, r, pl.b);
@@ -294,30 +313,27 @@ __global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_at
     const int pos0 = (blk0 + wave + 4 * i) * 32;
     f32x4 sc[QT][2];
 #pragma unroll
-    for (int qt = 0; qt < QT; ++qt) block_scores<T, DH>(kf, qf[qt], sc[qt]);
+    for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+      for (int pt = 0; pt < 2; ++pt) {
+        sc[qt][pt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int dt = 0; dt < DH / 32; ++dt) sc[qt][pt] = mma8(sc[qt][pt], kf[pt][dt], qf[qt][dt]);
+      }
     const int next = seek(i + 1);
     if (next < nb) load_keys();
     const bool masked = pos0 + 31 > first || pos0 + 31 >= end || (window && pos0 <= last - window);
-    uint32_t vis[QT];
     if (masked) {
 #pragma unroll
-      for (int qt = 0; qt < QT; ++qt) vis[qt] = mask_scores(pos0, qpos[qt], window, end, grp, sc[qt]);
+      for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+        for (int pt = 0; pt < 2; ++pt) mask_scores(pos0 + pt * 16, qpos[qt], window, end, grp, sc[qt][pt]);
     }
 #pragma unroll
-    for (int qt = 0; qt < QT; ++qt) softmax_step<T, DH>(sc[qt], c_log2, ref[qt], l_run[qt], o[qt]);
+    for (int qt = 0; qt < QT; ++qt) softmax_step(sc[qt], c_log2, ref[qt], l_run[qt], o[qt]);
     if (masked) {
-      // Positions no row of the tile sees hold anything, and 0 x NaN is not 0.
-      bool odd = false;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool past = pos0 + (e < 4 ? grp * 4 + e : 16 + grp * 4 + e - 4) >= end;
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt) {
-          if (past) vf[dt].v[e] = from_f32<T>(0.f);
-          odd |= nonfinite(vf[dt].v[e]);
-        }
-      }
-      if (__ballot(odd)) infinite_values<T, DH, QT>(vf, vis, o);
+      for (int dt = 0; dt < ND; ++dt) clean_values(vf[dt], pos0, qpos, window, end, grp, o, dt);
     }
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
@@ -374,92 +390,281 @@ __global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_at
   }
   if (wave) return;
 #pragma unroll
-  for (int qt = 0; qt < QT; ++qt) {
-    const int row = row0 + qt * 16 + r16;
-    if (row >= nrows) continue;
-    if (pl.ranges > 1) {
-      const size_t at = (pl.slot + static_cast<long>(pl.range) * c.H) * TR + qt * 16 + r16;
-      if (grp == 0) part_ml[at] = make_float2(ref[qt], l_run[qt]);
-#pragma unroll
-      for (int dt = 0; dt < ND; ++dt)
-        *reinterpret_cast<f32x4*>(part_o + at * DH + dt * 16 + grp * 4) = o[qt][dt];
-    } else {
-      // A sum of zero: no visible position, or none with weight.
-      const float inv = l_run[qt] == 0.f ? 0.f : 1.f / l_run[qt];
-      T* dst = out + tok[qt] * ldo + head[qt] * DH + grp * 4;
-#pragma unroll
-      for (int dt = 0; dt < ND; ++dt) store4_any(dst + dt * 16, l_run[qt] == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[qt][dt] * inv);
-      if (lse && grp == 0)
-        lse[static_cast<size_t>(tok[qt]) * c.H * c.G + head[qt]] =
-            l_run[qt] == 0.f ? -INFINITY : 0.69314718f * ref[qt] + logf(l_run[qt]);
-    }
-  }
+  for (int qt = 0; qt < QT; ++qt)
+    if (row0 + qt * 16 + r16 < nrows)
+      write_row<T, DH>(c, k, pl, qt * 16 + r16, tok[qt], head[qt], grp, ref[qt], l_run[qt], o[qt], out, ldo, lse, part_o,
+                       part_ml);
 }
 
 // The ranges of a tile's rows joined: one wave per row.
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedView c, PagedRows r, int target, int tile_rows,
-                                                         int window, const float* __restrict__ part_o,
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedView c, PagedRows r, Class k, int window, const float* __restrict__ part_o,
                                                          const float2* __restrict__ part_ml, T* __restrict__ out,
                                                          int64_t ldo, float* __restrict__ lse) {
   __shared__ int words[2 * kMaxPagedB];
   Place pl;
-  if (!find_place(c, r, window, tile_rows, target, true, blockIdx.x, words, words + kMaxPagedB, nullptr, &pl)) return;
+  if (!find_place(c, r, window, k, true, blockIdx.x, words, words + kMaxPagedB, nullptr, &pl)) return;
   const SeqRows s = seq_rows(c, r, pl.b);
-  const int lane = threadIdx.x & 63, in = blockIdx.y * 4 + (threadIdx.x >> 6);
-  const int row = pl.tile * tile_rows + in;
-  if (row >= s.n * c.G) return;
-  const float2* ml = part_ml + pl.slot * tile_rows + in;
-  const float* po = part_o + (pl.slot * tile_rows + in) * DH + lane * (DH / 64);
-  const size_t step = static_cast<size_t>(c.H) * tile_rows;      // from range to range
-  float m = -INFINITY;
-  for (int i = lane; i < pl.ranges; i += 64) m = fmaxf(m, ml[i * step].x);
-  m = wave_max(m);
-  float l = 0.f, acc[DH / 64] = {};
-  if (m != -INFINITY) {
+  const int lane = threadIdx.x & 63;
+  const size_t step = static_cast<size_t>(c.H) * k.tile;         // from range to range
+  for (int in = blockIdx.y * 4 + (threadIdx.x >> 6); in < k.tile; in += 4 * gridDim.y) {
+    const int row = pl.tile * k.tile + in;
+    if (row >= s.n * c.G) return;
+    const float2* ml = part_ml + pl.slot * k.tile + in;
+    const float* po = part_o + (pl.slot * k.tile + in) * DH + lane * (DH / 64);
+    float m = -INFINITY;
+    for (int i = lane; i < pl.ranges; i += 64) m = fmaxf(m, ml[i * step].x);
+    m = wave_max(m);
+    float l = 0.f, acc[DH / 64] = {};
+    if (m != -INFINITY) {
 #pragma unroll 8
-    for (int i = 0; i < pl.ranges; ++i) {
-      const float2 x = ml[i * step];
-      if (x.x == -INFINITY) continue;
-      const float w = fast_exp2(x.x - m);
-      l += w * x.y;
+      for (int i = 0; i < pl.ranges; ++i) {
+        const float2 x = ml[i * step];
+        if (x.x == -INFINITY) continue;
+        const float w = fast_exp2(x.x - m);
+        l += w * x.y;
 #pragma unroll
-      for (int d = 0; d < DH / 64; ++d) acc[d] += w * po[i * step * DH + d];
+        for (int d = 0; d < DH / 64; ++d) acc[d] += w * po[i * step * DH + d];
+      }
+    }
+    const int t = row / c.G, tok = s.r0 + t, head = pl.kvh * c.G + row - t * c.G;
+#pragma unroll
+    for (int d = 0; d < DH / 64; ++d)
+      out[tok * ldo + head * DH + lane * (DH / 64) + d] = from_f32<T>(l == 0.f ? 0.f : acc[d] / l);
+    if (lse && lane == 0)
+      lse[static_cast<size_t>(tok) * c.H * c.G + head] = l == 0.f ? -INFINITY : 0.69314718f * m + logf(l);
+  }
+}
+
+// Sequences with many query rows: NW waves of 16 QT rows each against the
+// range's blocks, 64 positions at a time through LDS. The page tiles are
+// copied there as they lie (global_load_lds, a KiB per wave and copy: no
+// registers, no bank conflicts on the way back), the next 64 positions while
+// these are computed. What bounds it is the matrix units (QT 64-cycle products
+// per KiB of LDS read) with the softmax's vector work beside them, which the
+// second wave of every SIMD covers.
+__device__ __forceinline__ void copy_to_lds(const void* src, uint32_t lds) {
+  // Untracked by the compiler's wait counts: it would make every LDS read wait
+  // for the copies of the other stage too.
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(lds) : "memory");
+}
+
+template <typename T, int DH, int QT, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, PagedRows r, Class k,
+                                                                const T* __restrict__ q, int64_t ldq, float scale,
+                                                                int window, T* __restrict__ out, int64_t ldo,
+                                                                float* __restrict__ lse, float* __restrict__ part_o,
+                                                                float2* __restrict__ part_ml, int* err) {
+  constexpr int ND = DH / 16, WR = 16 * QT;
+  constexpr int NB = sizeof(T) == 2 ? 2 : 1;                       // blocks per stage
+  constexpr int kTile = 32 * DH;                                   // elements of a block's keys or values
+  constexpr int kCopies = kTile * static_cast<int>(sizeof(T)) / 1024;   // of one KiB
+  static_assert(2 * NB * kCopies % NW == 0, "whole copies per wave");
+  __shared__ __align__(1024) T stage[2][NB][2][kTile];
+  static_assert(sizeof(stage) >= 2 * kMaxPagedB * sizeof(int), "the plan's words");
+  int* words = reinterpret_cast<int*>(stage);
+  Place pl;
+  if (!find_place(c, r, window, k, false, blockIdx.x, words, words + kMaxPagedB, err, &pl)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r16 = lane & 15, grp = lane >> 4;
+  const SeqRows s = seq_rows(c, r, pl.b);
+  const int cap = c.max_pages << c.page_log2;
+  // The last tiles of a prompt see most: they go first.
+  const int nrows = s.n * c.G, ntiles = (nrows + k.tile - 1) / k.tile;
+  const int tile = pl.ranges > 1 ? pl.tile : ntiles - 1 - pl.tile;
+  const int row0 = tile * k.tile, wrow0 = row0 + wave * WR;
+  const int first = s.p0 + row0 / c.G, last = s.p0 + (min(row0 + k.tile, nrows) - 1) / c.G;
+  const int end = min(max(last + 1, 0), cap);
+  const int lo = window ? min(max(first - window + 1, 0), end) : 0;
+  const int base = (window ? min(max(s.p0 - window + 1, 0), min(max(s.p0 + s.n, 0), cap)) : 0) / 32;
+  const int blk0 = max(base + pl.range * pl.per, lo / 32), blk1 = min(base + (pl.range + 1) * pl.per, (end + 31) / 32);
+  // The same of this wave's rows; none: wlast < 0.
+  const int wfirst = s.p0 + wrow0 / c.G, wlast = wrow0 < nrows ? s.p0 + (min(wrow0 + WR, nrows) - 1) / c.G : -1;
+  const float c_log2 = scale * 1.4426950408889634f;
+
+  Frag<T> qf[QT][DH / 32];
+  int qpos[QT];
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) {
+    const int row = wrow0 + qt * 16 + r16;
+    const bool valid = row < nrows;
+    const int t = valid ? row / c.G : 0;
+    qpos[qt] = valid ? s.p0 + t : -1;
+    const T* src = q + (s.r0 + t) * ldq + (pl.kvh * c.G + (valid ? row - t * c.G : 0)) * DH + grp * 8;
+#pragma unroll
+    for (int dt = 0; dt < DH / 32; ++dt) qf[qt][dt] = valid ? load_frag_any(src + dt * 32) : Frag<T>::zero();
+  }
+  float ref[QT], l_run[QT];
+  f32x4 o[QT][ND];
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) {
+    ref[qt] = -INFINITY;
+    l_run[qt] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const int32_t* tab = c.table + static_cast<size_t>(pl.b) * c.max_pages;
+  const size_t area = static_cast<size_t>(DH) << c.page_log2;
+  const int in_page = (1 << c.page_log2) - 1;
+  int id = -1, id0 = -64;                          // the pages of blocks id0 .. id0 + 63, one a lane
+  auto page_of = [&](int blk) {
+    if (blk - id0 >= 64 || id0 < 0) {
+      id0 = blk;
+      id = -1;
+      if (blk + lane < blk1) {
+        id = tab[(blk + lane) >> (c.page_log2 - 5)];
+        if (id < 0 || id >= c.n_pages) {
+          atomicOr(err, kErrBadPage);
+          id = -1;
+        }
+      }
+    }
+    return __builtin_amdgcn_readlane(id, blk - id0);
+  };
+  // Copy the blocks from blk on (up to NB) into stage b; bit h of the result: block h is there.
+  auto fetch = [&](int blk, int b) {
+    uint32_t there = 0;
+    size_t off[NB];
+#pragma unroll
+    for (int h = 0; h < NB; ++h) {
+      const int page = blk + h < blk1 ? page_of(blk + h) : -1;
+      off[h] = (static_cast<size_t>(max(page, 0)) * c.H + pl.kvh) * area + static_cast<size_t>((blk + h) * 32 & in_page) * DH;
+      there |= page >= 0 ? 1u << h : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < 2 * NB * kCopies / NW; ++j) {
+      const int n = wave * (2 * NB * kCopies / NW) + j;
+      const int h = n / (2 * kCopies), kv = n / kCopies & 1, at = n % kCopies;
+      if (!(there >> h & 1)) continue;
+      const char* src = static_cast<const char*>(kv ? c.v : c.k) + (h ? off[NB - 1] : off[0]) * sizeof(T) + at * 1024 + lane * 16;
+      copy_to_lds(src, static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&stage[b][h][kv][0])) + at * 1024);
+    }
+    return there;
+  };
+  __syncthreads();                                 // the plan's words have been read
+  uint32_t there = blk0 < blk1 ? fetch(blk0, 0) : 0;
+  int b = 0;
+  for (int blk = blk0; blk < blk1; blk += NB, b ^= 1) {
+    // This stage's copies have landed, and the other one's reads are over, in every wave.
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const uint32_t next = blk + NB < blk1 ? fetch(blk + NB, b ^ 1) : 0;
+    const int pos0 = blk * 32;
+    bool on[NB];
+    bool any = false;
+#pragma unroll
+    for (int h = 0; h < NB; ++h) {
+      on[h] = (there >> h & 1) && pos0 + h * 32 <= wlast && !(window && pos0 + h * 32 + 31 <= wfirst - window);
+      any |= on[h];
+    }
+    there = next;
+    if (!any) continue;
+    f32x4 sc[QT][2 * NB];
+#pragma unroll
+    for (int h = 0; h < NB; ++h)
+#pragma unroll
+      for (int pt = 0; pt < 2; ++pt) {
+        if (on[h]) {
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt) sc[qt][h * 2 + pt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int dt = 0; dt < DH / 32; ++dt) {
+            const Frag<T> kf = load_frag(&stage[b][h][0][((pt * (DH / 32) + dt) * 64 + lane) * 8]);
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt) sc[qt][h * 2 + pt] = mma8(sc[qt][h * 2 + pt], kf, qf[qt][dt]);
+          }
+        } else {
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt) sc[qt][h * 2 + pt] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        }
+      }
+    const bool masked = pos0 + NB * 32 - 1 > wfirst || pos0 + NB * 32 - 1 >= end || (window && pos0 <= wlast - window);
+    if (masked) {
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+        for (int pt = 0; pt < 2 * NB; ++pt) mask_scores(pos0 + pt * 16, qpos[qt], window, end, grp, sc[qt][pt]);
+    }
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) softmax_step(sc[qt], c_log2, ref[qt], l_run[qt], o[qt]);
+    // Weights rounded once to the type (bf16: half a step, 2^-8 of each, which
+    // averages out over a row like the values' own rounding; a second product
+    // of what is left off would cost half as much again).
+#pragma unroll
+    for (int h = 0; h < NB; ++h) {
+      if (!on[h]) continue;
+      Frag<T> pf[QT];
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pf[qt].v[e] = from_f32<T>(sc[qt][h * 2 + (e >> 2)][e & 3]);
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) {
+        Frag<T> vf = load_frag(&stage[b][h][1][(dt * 64 + lane) * 8]);
+        if (masked) clean_values(vf, pos0 + h * 32, qpos, window, end, grp, o, dt);
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) o[qt][dt] = mma8(o[qt][dt], vf, pf[qt]);
+      }
     }
   }
-  const int t = row / c.G, tok = s.r0 + t, head = pl.kvh * c.G + row - t * c.G;
 #pragma unroll
-  for (int d = 0; d < DH / 64; ++d)
-    out[tok * ldo + head * DH + lane * (DH / 64) + d] = from_f32<T>(l == 0.f ? 0.f : acc[d] / l);
-  if (lse && lane == 0)
-    lse[static_cast<size_t>(tok) * c.H * c.G + head] = l == 0.f ? -INFINITY : 0.69314718f * m + logf(l);
+  for (int qt = 0; qt < QT; ++qt) {
+    l_run[qt] += __shfl_xor(l_run[qt], 16);
+    l_run[qt] += __shfl_xor(l_run[qt], 32);
+    const int row = wrow0 + qt * 16 + r16;
+    if (row < nrows) {
+      const int t = row / c.G;
+      write_row<T, DH>(c, k, pl, row - row0, s.r0 + t, pl.kvh * c.G + row - t * c.G, grp, ref[qt], l_run[qt], o[qt], out,
+                       ldo, lse, part_o, part_ml);
+    }
+  }
 }
 
 template <typename T, int DH>
 static hipError_t attn_t(const PagedView& c, const PagedRows& r, const PagedPlan& p, const void* q, int64_t ldq,
-                         float scale, int window, void* out, int64_t ldo, float* lse, float* part_o, float2* part_ml,
-                         int* err, hipStream_t st) {
-  auto kern = p.qt == 1   ? paged_attn_kernel<T, DH, 1>
-              : p.qt == 2 ? paged_attn_kernel<T, DH, 2>
-              : p.qt == 3 ? paged_attn_kernel<T, DH, 3>
-                          : paged_attn_kernel<T, DH, 4>;
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(p.items)), dim3(256), 0, st, c, r, p.target,
-                     static_cast<const T*>(q), ldq, scale, window, static_cast<T*>(out), ldo, lse, part_o, part_ml, err);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.joins == 0) return e;
-  hipLaunchKernelGGL((paged_join_kernel<T, DH>), dim3(static_cast<unsigned>(p.joins), 4 * p.qt), dim3(256), 0, st, c, r,
-                     p.target, 16 * p.qt, window, part_o, part_ml, static_cast<T*>(out), ldo, lse);
-  return hipGetLastError();
+                         float scale, int window, void* out, int64_t ldo, float* lse, char* ws, int* err,
+                         hipStream_t st) {
+  const T* qq = static_cast<const T*>(q);
+  T* oo = static_cast<T*>(out);
+  const Class few{p.few.tile, p.few.target, 0, p.limit}, many{p.many.tile, p.many.target, p.limit, INT32_MAX};
+  float *fo = reinterpret_cast<float*>(ws + p.few.o_off), *mo = reinterpret_cast<float*>(ws + p.many.o_off);
+  float2 *fm = reinterpret_cast<float2*>(ws + p.few.ml_off), *mm = reinterpret_cast<float2*>(ws + p.many.ml_off);
+  hipError_t e = hipSuccess;
+  if (p.many.items) {
+    hipLaunchKernelGGL((paged_many_kernel<T, DH, kManyQt, kManyWaves>), dim3(static_cast<unsigned>(p.many.items)),
+                       dim3(64 * kManyWaves), 0, st, c, r, many, qq, ldq, scale, window, oo, ldo, lse, mo, mm, err);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (p.few.items) {
+    auto kern = p.qt == 1   ? paged_few_kernel<T, DH, 1>
+                : p.qt == 2 ? paged_few_kernel<T, DH, 2>
+                : p.qt == 3 ? paged_few_kernel<T, DH, 3>
+                            : paged_few_kernel<T, DH, 4>;
+    hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(p.few.items)), dim3(256), 0, st, c, r, few, qq, ldq, scale,
+                       window, oo, ldo, lse, fo, fm, err);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (p.many.joins) {
+    hipLaunchKernelGGL((paged_join_kernel<T, DH>), dim3(static_cast<unsigned>(p.many.joins), 8), dim3(256),
+                       0, st, c, r, many, window, mo, mm, oo, ldo, lse);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (p.few.joins) {
+    hipLaunchKernelGGL((paged_join_kernel<T, DH>), dim3(static_cast<unsigned>(p.few.joins), p.few.tile / 8), dim3(256), 0,
+                       st, c, r, few, window, fo, fm, oo, ldo, lse);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 hipError_t launch_paged_attention(int dtype, const PagedView& c, const PagedRows& r, const PagedPlan& p, const void* q,
-                                  int64_t ldq, float scale, int window, void* out, int64_t ldo, float* lse,
-                                  float* part_o, float2* part_ml, int* err, hipStream_t st) {
+                                  int64_t ldq, float scale, int window, void* out, int64_t ldo, float* lse, char* ws,
+                                  int* err, hipStream_t st) {
   if (dtype == 1)
-    return c.DH == 128 ? attn_t<bf16, 128>(c, r, p, q, ldq, scale, window, out, ldo, lse, part_o, part_ml, err, st)
-                       : attn_t<bf16, 64>(c, r, p, q, ldq, scale, window, out, ldo, lse, part_o, part_ml, err, st);
-  return c.DH == 128 ? attn_t<float, 128>(c, r, p, q, ldq, scale, window, out, ldo, lse, part_o, part_ml, err, st)
-                     : attn_t<float, 64>(c, r, p, q, ldq, scale, window, out, ldo, lse, part_o, part_ml, err, st);
+    return c.DH == 128 ? attn_t<bf16, 128>(c, r, p, q, ldq, scale, window, out, ldo, lse, ws, err, st)
+                       : attn_t<bf16, 64>(c, r, p, q, ldq, scale, window, out, ldo, lse, ws, err, st);
+  return c.DH == 128 ? attn_t<float, 128>(c, r, p, q, ldq, scale, window, out, ldo, lse, ws, err, st)
+                     : attn_t<float, 64>(c, r, p, q, ldq, scale, window, out, ldo, lse, ws, err, st);
 }
 
 }  // namespace sps

@@ -281,27 +281,44 @@ sps_status check_paged_rows(const sps_paged_config& c, bool ragged, int rows, in
   return SPS_OK;
 }
 
-PagedPlan paged_plan(const sps_paged_config& c, int rows, int max_tokens) {
-  PagedPlan p{};
+namespace {
+// The class of sequences that have up to `most` query rows each; `at` is the
+// workspace's end so far.
+PagedClass paged_class(const sps_paged_config& c, int tile, int target, long rows, size_t* at) {
+  PagedClass k{};
   const int G = c.n_heads / c.n_kv_heads;
-  const long q = static_cast<long>(std::min(rows, max_tokens)) * G;
-  p.qt = q <= 48 ? static_cast<int>((q + 15) / 16) : 4;
-  p.target = 4 * kCUs;
-  const long tile = 16L * p.qt;
+  k.tile = tile;
+  k.target = target;
   // Every sequence's last tile may be partly filled.
-  const long tiles = (static_cast<long>(rows) * G / tile + std::min(c.B, rows)) * c.n_kv_heads;
+  const long tiles = (rows * G / tile + std::min<long>(c.B, rows)) * c.n_kv_heads;
   const long blocks = (static_cast<long>(c.max_pages) * c.page_size) / 32;
   const long ranges = (blocks + kPagedMinBlocks - 1) / kPagedMinBlocks;
   // A sequence of n blocks has at most n / per + 1 ranges, and per is at least
   // (all tiles' blocks) / target, so the ranges are at most target plus one a
   // tile; only tiles of two ranges or more leave partials, at most twice
   // their n / per.
-  p.items = std::min(tiles * ranges, tiles + p.target);
-  p.slots = ranges > 1 ? std::min(p.items, 2L * p.target) : 0;
-  p.joins = std::min(tiles, p.slots / 2);
-  p.o_off = 0;
-  p.ml_off = align256(static_cast<size_t>(p.slots) * tile * c.head_dim * 4);
-  p.total = p.ml_off + align256(static_cast<size_t>(p.slots) * tile * 8);
+  k.items = std::min(tiles * ranges, tiles + target);
+  k.slots = ranges > 1 ? std::min(k.items, 2L * target) : 0;
+  k.joins = std::min(tiles, k.slots / 2);
+  k.o_off = *at;
+  *at = align256(*at + static_cast<size_t>(k.slots) * tile * c.head_dim * 4);
+  k.ml_off = *at;
+  *at = align256(*at + static_cast<size_t>(k.slots) * tile * 8);
+  return k;
+}
+}  // namespace
+
+PagedPlan paged_plan(const sps_paged_config& c, bool ragged, int rows, int max_tokens) {
+  PagedPlan p{};
+  const int G = c.n_heads / c.n_kv_heads;
+  const long q = static_cast<long>(std::min(rows, max_tokens)) * G;
+  // Up to 64 query rows: one tile of the smallest size that holds them.
+  // Among prompts of a ragged batch, those of up to 8 tokens.
+  const long few = q <= 64 ? q : ragged ? 8L * G : 0;
+  p.qt = static_cast<int>(std::min<long>(4, (few + 15) / 16));
+  p.limit = 16 * p.qt;
+  if (p.qt) p.few = paged_class(c, 16 * p.qt, 4 * kCUs, rows, &p.total);
+  if (q > p.limit) p.many = paged_class(c, 16 * kManyQt * kManyWaves, 2 * kCUs, rows, &p.total);
   if (p.total == 0) p.total = 256;
   return p;
 }
@@ -310,11 +327,12 @@ size_t paged_workspace_bytes(const sps_paged_config* c, int rows, int max_tokens
   if (!valid_paged(c) || rows < 0 || max_tokens < 0 || rows > kMaxPagedRows || max_tokens > kMaxPagedRows ||
       (rows > 0 && max_tokens == 0))
     return 0;
-  // Calls with fewer tokens per sequence have smaller tiles and may have more of them.
+  // Calls with fewer tokens per sequence have other tiles and may have more of them.
   size_t most = 256;
   const int G = c->n_heads / c->n_kv_heads;
-  for (long q : {16L, 32L, 48L, static_cast<long>(kMaxPagedRows)})
-    most = std::max(most, paged_plan(*c, rows, static_cast<int>(std::max(1L, std::min<long>(max_tokens, q / G)))).total);
+  for (long q : {16L, 32L, 48L, 64L, static_cast<long>(kMaxPagedRows) * 1024})
+    for (bool ragged : {false, true})
+      most = std::max(most, paged_plan(*c, ragged, rows, static_cast<int>(std::max(1L, std::min<long>(max_tokens, q / G)))).total);
   return most;
 }
 

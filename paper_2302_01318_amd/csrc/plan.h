@@ -189,23 +189,29 @@ size_t paged_bytes(const sps_paged_config* c);
 // Whether a call's rows are ones the paged operators take (starts: ragged).
 sps_status check_paged_rows(const sps_paged_config& c, bool ragged, int rows, int max_tokens);
 
-// Attention over the pages. A work item is the tile of up to `tile` query
-// rows (a sequence's tokens x the query heads of one KV head) against a range
-// of 32-position blocks. Ranges are the same number of blocks for the whole
-// call, chosen on the device from the actual lengths so that there are about
-// `target` items, no fewer than kPagedMinBlocks each. Items whose rows have only one range
-// write the output; the others leave partials in at most `slots` slots of the
-// workspace, which a second launch joins.
-constexpr int kPagedMinBlocks = 8;     // 256 positions: two blocks per wave
-struct PagedPlan {
-  int qt;              // 16-row tiles per item
-  int target;          // items wanted
-  long items;          // most items there can be: the grid
-  long slots;          // most partials there can be
-  long joins;          // most (tile, KV head) pairs with partials
-  size_t o_off, ml_off, total;   // workspace: partial outputs, then (max, sum) pairs
+// Attention over the pages. A work item is a tile of up to `tile` query rows
+// (a sequence's tokens x the query heads of one KV head) against a range of
+// 32-position blocks. Ranges are the same number of blocks for all sequences
+// of a class, chosen on the device from the actual lengths so that there are
+// about `target` items, no fewer than kPagedMinBlocks each. Items whose rows
+// have only one range write the output; the others leave partials in at most
+// `slots` slots of the workspace, which a second launch joins. Sequences with
+// up to `limit` query rows are one class (their waves take different
+// positions, qt 16-row tiles each), those with more the other (their waves
+// take different rows).
+constexpr int kPagedMinBlocks = 8;     // 256 positions
+constexpr int kManyWaves = 8, kManyQt = 2;
+struct PagedClass {
+  int tile, target;
+  long items, slots, joins;            // the most there can be; items 0: no such sequence
+  size_t o_off, ml_off;                // workspace: partial outputs, (reference, sum) pairs
 };
-PagedPlan paged_plan(const sps_paged_config& c, int rows, int max_tokens);
+struct PagedPlan {
+  int qt, limit;
+  PagedClass few, many;
+  size_t total;
+};
+PagedPlan paged_plan(const sps_paged_config& c, bool ragged, int rows, int max_tokens);
 size_t paged_workspace_bytes(const sps_paged_config* c, int rows, int max_tokens);
 
 // Host-side check of the sampling parameters for a vocabulary of V.

@@ -717,15 +717,13 @@ sps_status sps_paged_attention(sps_paged_t kv, int32_t layer, const void* q, int
   if (!q || !out || q == out || !workspace || misaligned(q, c.dtype) || misaligned(out, c.dtype) ||
       reinterpret_cast<uintptr_t>(workspace) % 256)
     return SPS_E_INVALID;
-  const sps::PagedPlan p = sps::paged_plan(c, rows, max_tokens);
+  const sps::PagedPlan p = sps::paged_plan(c, starts != nullptr, rows, max_tokens);
   if (ws_bytes < p.total) return SPS_E_CAPACITY;
   int* err = device_error_ptr();
   if (!err) return SPS_E_HIP;
-  char* ws = static_cast<char*>(workspace);
   SPS_HIP(sps::launch_paged_attention(c.dtype, paged_view(kv, layer), {starts, rows, max_tokens, pos_offset}, p, q,
-                                      q_stride, scale, window, out, out_stride, lse,
-                                      reinterpret_cast<float*>(ws + p.o_off), reinterpret_cast<float2*>(ws + p.ml_off),
-                                      err, as_stream(stream)));
+                                      q_stride, scale, window, out, out_stride, lse, static_cast<char*>(workspace), err,
+                                      as_stream(stream)));
   return SPS_OK;
 }
 
