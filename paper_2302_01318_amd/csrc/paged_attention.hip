@@ -8,6 +8,8 @@
 // order is made for): both tiles go from the page straight into registers, a
 // KiB per wave and load. The waves' (O, max, sum) meet in LDS; ranges of one
 // tile meet in a second launch.
+#include <type_traits>
+
 #include "paged.h"
 
 namespace sps {
@@ -100,40 +102,52 @@ __device__ __forceinline__ void mask_scores(int pos0, int qpos, int window, int 
   }
 }
 
-// Online softmax step on one tile's scores. The reference that is taken off
-// the scaled scores (ref, in units of log2) follows the running maximum only
-// once that is kLag above it: weights are at most 2^kLag instead of 1, which
-// fp32 sums and bf16 weights hold as precisely, and the accumulators are
-// rescaled a few times per row instead of in nearly every block. Each lane
-// sums its own positions' weights.
+// Online softmax of one query row, spread over the four lanes with its column.
+// The reference `off` that is taken off the scaled scores (in units of log2)
+// follows the running maximum only once that is kLag above it: weights are at
+// most 2^kLag instead of 1, which fp32 sums and bf16 weights hold as precisely,
+// and the accumulators are rescaled a few times per row instead of in nearly
+// every block. Each lane sums its own positions' weights.
 constexpr float kLag = 8.f;
+struct RowSoftmax {
+  float off = 0.f;
+  float lim = -INFINITY;   // kLag once there is a reference
+  float sum = 0.f;
+  __device__ float ref() const { return lim == -INFINITY ? -INFINITY : off; }
+};
+// s: scores in, weights out (NP tiles of 16 positions).
 template <int NP, int ND>
-__device__ __forceinline__ void softmax_step(f32x4 (&s)[NP], float c_log2, float& ref, float& l_run, f32x4 (&o)[ND]) {
+__device__ __forceinline__ void softmax_step(f32x4 (&s)[NP], float c_log2, RowSoftmax& w, f32x4 (&o)[ND]) {
   float mx = -INFINITY;
 #pragma unroll
-  for (int pt = 0; pt < NP; ++pt) mx = fmaxf(mx, fmaxf(fmaxf(s[pt][0], s[pt][1]), fmaxf(s[pt][2], s[pt][3])));
-  mx *= c_log2;
-  if (__ballot(mx > ref + kLag)) {
+  for (int pt = 0; pt < NP; ++pt) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s[pt][r] = fmaf(s[pt][r], c_log2, -w.off);
+    mx = fmaxf(fmaxf(fmaxf(fmaxf(mx, s[pt][0]), s[pt][1]), s[pt][2]), s[pt][3]);
+  }
+  if (__ballot(mx > w.lim)) {
     mx = fmaxf(mx, __shfl_xor(mx, 16));
     mx = fmaxf(mx, __shfl_xor(mx, 32));
-    if (mx > ref + kLag) {                         // alike in the four lanes of a row
-      const float alpha = fast_exp2(ref - mx);     // 0 for the row's first reference
-      ref = mx;
-      l_run *= alpha;
+    if (mx > w.lim) {                              // alike in the four lanes of a row
+      const float alpha = w.lim == -INFINITY ? 0.f : fast_exp2(-mx);   // nothing summed yet: 0
+      w.off += mx;
+      w.lim = kLag;
+      w.sum *= alpha;
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) o[dt] *= alpha;
+#pragma unroll
+      for (int pt = 0; pt < NP; ++pt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[pt][r] -= mx;
     }
   }
-  const float off = ref == -INFINITY ? 0.f : ref;
-  float ps = 0.f;
 #pragma unroll
   for (int pt = 0; pt < NP; ++pt)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      s[pt][r] = fast_exp2(fmaf(s[pt][r], c_log2, -off));
-      ps += s[pt][r];
+      s[pt][r] = fast_exp2(s[pt][r]);
+      w.sum += s[pt][r];
     }
-  l_run += ps;
 }
 
 // Values of a block in which some row of the tile does not see some position:
@@ -247,15 +261,12 @@ __global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_fe
     for (int dt = 0; dt < DH / 32; ++dt)
       qf[qt][dt] = valid ? load_frag_any(q + tok[qt] * ldq + head[qt] * DH + dt * 32 + grp * 8) : Frag<T>::zero();
   }
-  float ref[QT], l_run[QT];
+  RowSoftmax w[QT];
   f32x4 o[QT][ND];
 #pragma unroll
-  for (int qt = 0; qt < QT; ++qt) {
-    ref[qt] = -INFINITY;
-    l_run[qt] = 0.f;
+  for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
 
   // This wave's blocks are blk0 + wave + 4 i; the pages of 64 of them at a
   // time. The next block's keys are asked for once the scores are done with
@@ -330,7 +341,7 @@ __global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_fe
         for (int pt = 0; pt < 2; ++pt) mask_scores(pos0 + pt * 16, qpos[qt], window, end, grp, sc[qt][pt]);
     }
 #pragma unroll
-    for (int qt = 0; qt < QT; ++qt) softmax_step(sc[qt], c_log2, ref[qt], l_run[qt], o[qt]);
+    for (int qt = 0; qt < QT; ++qt) softmax_step(sc[qt], c_log2, w[qt], o[qt]);
     if (masked) {
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) clean_values(vf[dt], pos0, qpos, window, end, grp, o, dt);
@@ -357,10 +368,12 @@ __global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_fe
   }
 
   // Waves 2, 3 into 0, 1, then 1 into 0.
+  float ref[QT], sum[QT];
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {
-    l_run[qt] += __shfl_xor(l_run[qt], 16);
-    l_run[qt] += __shfl_xor(l_run[qt], 32);
+    ref[qt] = w[qt].ref();
+    sum[qt] = w[qt].sum + __shfl_xor(w[qt].sum, 16);
+    sum[qt] += __shfl_xor(sum[qt], 32);
   }
   __syncthreads();                                 // the plan's words have been read
 #pragma unroll
@@ -368,7 +381,7 @@ __global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_fe
     if (wave >= half && wave < 2 * half) {
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
-        sml[((wave - half) * QT + qt) * 64 + lane] = make_float2(ref[qt], l_run[qt]);
+        sml[((wave - half) * QT + qt) * 64 + lane] = make_float2(ref[qt], sum[qt]);
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) sm[(((wave - half) * QT + qt) * ND + dt) * 64 + lane] = o[qt][dt];
       }
@@ -381,7 +394,7 @@ __global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_fe
         const float m = fmaxf(ref[qt], ml.x), mu = m == -INFINITY ? 0.f : m;
         const float a = fast_exp2(ref[qt] - mu), b = fast_exp2(ml.x - mu);
         ref[qt] = m;
-        l_run[qt] = a * l_run[qt] + b * ml.y;
+        sum[qt] = a * sum[qt] + b * ml.y;
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) o[qt][dt] = a * o[qt][dt] + b * sm[((wave * QT + qt) * ND + dt) * 64 + lane];
       }
@@ -392,7 +405,7 @@ __global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_fe
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt)
     if (row0 + qt * 16 + r16 < nrows)
-      write_row<T, DH>(c, k, pl, qt * 16 + r16, tok[qt], head[qt], grp, ref[qt], l_run[qt], o[qt], out, ldo, lse, part_o,
+      write_row<T, DH>(c, k, pl, qt * 16 + r16, tok[qt], head[qt], grp, ref[qt], sum[qt], o[qt], out, ldo, lse, part_o,
                        part_ml);
 }
 
@@ -494,15 +507,12 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
 #pragma unroll
     for (int dt = 0; dt < DH / 32; ++dt) qf[qt][dt] = valid ? load_frag_any(src + dt * 32) : Frag<T>::zero();
   }
-  float ref[QT], l_run[QT];
+  RowSoftmax w[QT];
   f32x4 o[QT][ND];
 #pragma unroll
-  for (int qt = 0; qt < QT; ++qt) {
-    ref[qt] = -INFINITY;
-    l_run[qt] = 0.f;
+  for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
 
   const int32_t* tab = c.table + static_cast<size_t>(pl.b) * c.max_pages;
   const size_t area = static_cast<size_t>(DH) << c.page_log2;
@@ -550,71 +560,72 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     const uint32_t next = blk + NB < blk1 ? fetch(blk + NB, b ^ 1) : 0;
     const int pos0 = blk * 32;
-    bool on[NB];
-    bool any = false;
-#pragma unroll
-    for (int h = 0; h < NB; ++h) {
-      on[h] = (there >> h & 1) && pos0 + h * 32 <= wlast && !(window && pos0 + h * 32 + 31 <= wfirst - window);
-      any |= on[h];
-    }
-    there = next;
-    if (!any) continue;
-    f32x4 sc[QT][2 * NB];
+    uint32_t on = 0;                               // blocks this wave's rows see anything of
 #pragma unroll
     for (int h = 0; h < NB; ++h)
+      on |= pos0 + h * 32 <= wlast && !(window && pos0 + h * 32 + 31 <= wfirst - window) ? there & 1u << h : 0;
+    there = next;
+    if (!on) continue;
+    const bool all = on == (1u << NB) - 1 && pos0 + NB * 32 - 1 <= min(wfirst, end - 1) && !(window && pos0 <= wlast - window);
+    // One straight run over the stage where every row sees all of it; else
+    // block by block.
+    auto step = [&](auto whole, int h0) {
+      constexpr bool kWhole = decltype(whole)::value;
+      constexpr int NH = kWhole ? NB : 1;
+      const T(*st)[2][kTile] = &stage[b][h0];
+      f32x4 sc[QT][2 * NH];
 #pragma unroll
-      for (int pt = 0; pt < 2; ++pt) {
-        if (on[h]) {
+      for (int pt = 0; pt < 2 * NH; ++pt) {
 #pragma unroll
-          for (int qt = 0; qt < QT; ++qt) sc[qt][h * 2 + pt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int qt = 0; qt < QT; ++qt) sc[qt][pt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int dt = 0; dt < DH / 32; ++dt) {
-            const Frag<T> kf = load_frag(&stage[b][h][0][((pt * (DH / 32) + dt) * 64 + lane) * 8]);
+        for (int dt = 0; dt < DH / 32; ++dt) {
+          const Frag<T> kf = load_frag(&st[pt >> 1][0][(((pt & 1) * (DH / 32) + dt) * 64 + lane) * 8]);
 #pragma unroll
-            for (int qt = 0; qt < QT; ++qt) sc[qt][h * 2 + pt] = mma8(sc[qt][h * 2 + pt], kf, qf[qt][dt]);
-          }
-        } else {
+          for (int qt = 0; qt < QT; ++qt) sc[qt][pt] = mma8(sc[qt][pt], kf, qf[qt][dt]);
+        }
+        if (!kWhole) {
 #pragma unroll
-          for (int qt = 0; qt < QT; ++qt) sc[qt][h * 2 + pt] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          for (int qt = 0; qt < QT; ++qt) mask_scores(pos0 + (h0 * 2 + pt) * 16, qpos[qt], window, end, grp, sc[qt][pt]);
         }
       }
-    const bool masked = pos0 + NB * 32 - 1 > wfirst || pos0 + NB * 32 - 1 >= end || (window && pos0 <= wlast - window);
-    if (masked) {
 #pragma unroll
-      for (int qt = 0; qt < QT; ++qt)
+      for (int qt = 0; qt < QT; ++qt) softmax_step(sc[qt], c_log2, w[qt], o[qt]);
+      // Weights rounded once to the type (bf16: half a step, 2^-8 of each, which
+      // averages out over a row like the values' own rounding; a second product
+      // of what is left off would cost half as much again).
 #pragma unroll
-        for (int pt = 0; pt < 2 * NB; ++pt) mask_scores(pos0 + pt * 16, qpos[qt], window, end, grp, sc[qt][pt]);
-    }
+      for (int h = 0; h < NH; ++h) {
+        Frag<T> pf[QT];
 #pragma unroll
-    for (int qt = 0; qt < QT; ++qt) softmax_step(sc[qt], c_log2, ref[qt], l_run[qt], o[qt]);
-    // Weights rounded once to the type (bf16: half a step, 2^-8 of each, which
-    // averages out over a row like the values' own rounding; a second product
-    // of what is left off would cost half as much again).
+        for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
-    for (int h = 0; h < NB; ++h) {
-      if (!on[h]) continue;
-      Frag<T> pf[QT];
+          for (int e = 0; e < 8; ++e) pf[qt].v[e] = from_f32<T>(sc[qt][h * 2 + (e >> 2)][e & 3]);
 #pragma unroll
-      for (int qt = 0; qt < QT; ++qt)
+        for (int dt = 0; dt < ND; ++dt) {
+          Frag<T> vf = load_frag(&st[h][1][(dt * 64 + lane) * 8]);
+          if (!kWhole) clean_values(vf, pos0 + h0 * 32, qpos, window, end, grp, o, dt);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) pf[qt].v[e] = from_f32<T>(sc[qt][h * 2 + (e >> 2)][e & 3]);
-#pragma unroll
-      for (int dt = 0; dt < ND; ++dt) {
-        Frag<T> vf = load_frag(&stage[b][h][1][(dt * 64 + lane) * 8]);
-        if (masked) clean_values(vf, pos0 + h * 32, qpos, window, end, grp, o, dt);
-#pragma unroll
-        for (int qt = 0; qt < QT; ++qt) o[qt][dt] = mma8(o[qt][dt], vf, pf[qt]);
+          for (int qt = 0; qt < QT; ++qt) o[qt][dt] = mma8(o[qt][dt], vf, pf[qt]);
+        }
       }
+    };
+    if (all) {
+      step(std::true_type{}, 0);
+    } else {
+#pragma unroll 1
+      for (int h = 0; h < NB; ++h)
+        if (on >> h & 1) step(std::false_type{}, h);
     }
   }
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {
-    l_run[qt] += __shfl_xor(l_run[qt], 16);
-    l_run[qt] += __shfl_xor(l_run[qt], 32);
+    float sum = w[qt].sum + __shfl_xor(w[qt].sum, 16);
+    sum += __shfl_xor(sum, 32);
     const int row = wrow0 + qt * 16 + r16;
     if (row < nrows) {
       const int t = row / c.G;
-      write_row<T, DH>(c, k, pl, row - row0, s.r0 + t, pl.kvh * c.G + row - t * c.G, grp, ref[qt], l_run[qt], o[qt], out,
+      write_row<T, DH>(c, k, pl, row - row0, s.r0 + t, pl.kvh * c.G + row - t * c.G, grp, w[qt].ref(), sum, o[qt], out,
                        ldo, lse, part_o, part_ml);
     }
   }
