@@ -14,6 +14,20 @@
 
 namespace sps {
 
+// A value that is the same in every lane, in a scalar register.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ const char* uniform(const char* p) {
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = uniform(static_cast<int>(x)), hi = uniform(static_cast<int>(x >> 32));
+  return reinterpret_cast<const char*>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+__device__ __forceinline__ SeqRows uniform(SeqRows s) {
+  s.r0 = uniform(s.r0);
+  s.n = uniform(s.n);
+  s.p0 = uniform(s.p0);
+  return s;
+}
+
 // Where an item, or a (tile, KV head) with several ranges, belongs.
 struct Place {
   int b, tile, range, ranges, kvh;
@@ -32,7 +46,7 @@ struct Class {
 // `idx`. Every work-group of both launches computes the same plan from the
 // same lengths. Returns false past the last one.
 __device__ __forceinline__ bool find_place(const PagedView& c, const PagedRows& r, int window, const Class& k,
-                                           bool join, long idx, int* s_tiles, int* s_blocks, int* err, Place* out) {
+                                           bool join, uint32_t idx, int* s_tiles, int* s_blocks, int* err, Place* out) {
   const int lane = threadIdx.x & 63;
   const int cap = c.max_pages << c.page_log2;
   for (int b = threadIdx.x; b < c.B; b += blockDim.x) {
@@ -48,9 +62,8 @@ __device__ __forceinline__ bool find_place(const PagedView& c, const PagedRows& 
   uint64_t all = 0;
   for (int b0 = 0; b0 < c.B; b0 += 64)
     all += wave_sum_u64(b0 + lane < c.B ? static_cast<uint64_t>(s_tiles[b0 + lane]) * s_blocks[b0 + lane] : 0);
-  const int per = max(kPagedMinBlocks, static_cast<int>(ceil(static_cast<double>(all) * c.H / k.target)));
-  const int h = static_cast<int>(idx % c.H);
-  const uint32_t want = static_cast<uint32_t>(idx / c.H);
+  const int per = uniform(max(kPagedMinBlocks, static_cast<int>(ceil(static_cast<double>(all) * c.H / k.target))));
+  const int want = uniform(static_cast<int>(idx) / c.H), h = static_cast<int>(idx) - want * c.H;
   uint64_t before = 0;                             // (items or joins) << 32 | slots, per KV head
   for (int b0 = 0; b0 < c.B; b0 += 64) {
     const int b = b0 + lane;
@@ -59,18 +72,18 @@ __device__ __forceinline__ bool find_place(const PagedView& c, const PagedRows& 
     const uint32_t slots = ranges > 1 ? tiles * ranges : 0;
     const uint32_t mine = join ? (ranges > 1 ? tiles : 0) : tiles * ranges;
     const uint64_t incl = wave_incl_scan_u64(static_cast<uint64_t>(mine) << 32 | slots) + before;
-    const uint64_t hit = __ballot(want < static_cast<uint32_t>(incl >> 32));
+    const uint64_t hit = __ballot(want < static_cast<int>(incl >> 32));
     if (hit) {
       const int src = __ffsll(static_cast<unsigned long long>(hit)) - 1;
       const uint64_t inc = readlane_u64(incl, src);
       const int m = __builtin_amdgcn_readlane(static_cast<int>(mine), src);
       const int sl = __builtin_amdgcn_readlane(static_cast<int>(slots), src);
       const int nr = __builtin_amdgcn_readlane(static_cast<int>(ranges), src);
-      const int at = static_cast<int>(want - (static_cast<uint32_t>(inc >> 32) - m));
-      out->b = b0 + src;
+      const int at = static_cast<int>(want - (static_cast<int>(inc >> 32) - m));
+      out->b = uniform(b0 + src);
       out->ranges = nr;
-      out->tile = join ? at : at / nr;
-      out->range = join ? 0 : at % nr;
+      out->tile = join ? at : uniform(at / nr);
+      out->range = join ? 0 : at - out->tile * nr;
       out->kvh = h;
       out->per = per;
       const uint32_t slot0 = static_cast<uint32_t>(inc) - sl;
@@ -115,9 +128,10 @@ struct RowSoftmax {
   float sum = 0.f;
   __device__ float ref() const { return lim == -INFINITY ? -INFINITY : off; }
 };
-// s: scores in, weights out (NP tiles of 16 positions).
-template <int NP, int ND>
-__device__ __forceinline__ void softmax_step(f32x4 (&s)[NP], float c_log2, RowSoftmax& w, f32x4 (&o)[ND]) {
+// Scores of NP tiles of 16 positions scaled and without the reference;
+// returns the largest of the lane's.
+template <int NP>
+__device__ __forceinline__ float scale_scores(f32x4 (&s)[NP], float c_log2, const RowSoftmax& w) {
   float mx = -INFINITY;
 #pragma unroll
   for (int pt = 0; pt < NP; ++pt) {
@@ -125,22 +139,41 @@ __device__ __forceinline__ void softmax_step(f32x4 (&s)[NP], float c_log2, RowSo
     for (int r = 0; r < 4; ++r) s[pt][r] = fmaf(s[pt][r], c_log2, -w.off);
     mx = fmaxf(fmaxf(fmaxf(fmaxf(mx, s[pt][0]), s[pt][1]), s[pt][2]), s[pt][3]);
   }
-  if (__ballot(mx > w.lim)) {
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    if (mx > w.lim) {                              // alike in the four lanes of a row
-      const float alpha = w.lim == -INFINITY ? 0.f : fast_exp2(-mx);   // nothing summed yet: 0
-      w.off += mx;
-      w.lim = kLag;
-      w.sum *= alpha;
+  return mx;
+}
+// The same with a new reference where one is due; all QT rows of the lane
+// together, so that one branch skips the rescaling.
+template <int QT, int NP, int ND>
+__device__ __forceinline__ void softmax_scale(f32x4 (&s)[QT][NP], float c_log2, RowSoftmax (&w)[QT], f32x4 (&o)[QT][ND]) {
+  float mx[QT];
+  bool up = false;
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt) o[dt] *= alpha;
-#pragma unroll
-      for (int pt = 0; pt < NP; ++pt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s[pt][r] -= mx;
-    }
+  for (int qt = 0; qt < QT; ++qt) {
+    mx[qt] = scale_scores(s[qt], c_log2, w[qt]);
+    up |= mx[qt] > w[qt].lim;
   }
+  if (!__ballot(up)) return;
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) {
+    float m = fmaxf(mx[qt], __shfl_xor(mx[qt], 16));
+    m = fmaxf(m, __shfl_xor(m, 32));
+    const bool mine = m > w[qt].lim;               // alike in the four lanes of a row
+    // Nothing summed yet: 0.
+    const float alpha = !mine ? 1.f : w[qt].lim == -INFINITY ? 0.f : fast_exp2(-m);
+    m = mine ? m : 0.f;
+    w[qt].off += m;
+    w[qt].lim = mine ? kLag : w[qt].lim;
+    w[qt].sum *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) o[qt][dt] *= alpha;
+#pragma unroll
+    for (int pt = 0; pt < NP; ++pt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[qt][pt][r] -= m;
+  }
+}
+template <int NP>
+__device__ __forceinline__ void softmax_weights(f32x4 (&s)[NP], RowSoftmax& w) {
 #pragma unroll
   for (int pt = 0; pt < NP; ++pt)
 #pragma unroll
@@ -234,13 +267,13 @@ __global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_fe
   int* s_tiles = reinterpret_cast<int*>(sm);
   Place pl;
   if (!find_place(c, r, window, k, false, blockIdx.x, s_tiles, s_tiles + kMaxPagedB, err, &pl)) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int r16 = lane & 15, grp = lane >> 4;
-  const SeqRows s = seq_rows(c, r, pl.b);
+  const SeqRows s = uniform(seq_rows(c, r, pl.b));
   const int cap = c.max_pages << c.page_log2;
   const int nrows = s.n * c.G, row0 = pl.tile * TR;
   // Positions of the tile's first and last token, and what they see.
-  const int first = s.p0 + row0 / c.G, last = s.p0 + (min(row0 + TR, nrows) - 1) / c.G;
+  const int first = s.p0 + uniform(row0 / c.G), last = s.p0 + uniform((min(row0 + TR, nrows) - 1) / c.G);
   const int end = min(max(last + 1, 0), cap);
   const int lo = window ? min(max(first - window + 1, 0), end) : 0;
   const int base = (window ? min(max(s.p0 - window + 1, 0), min(max(s.p0 + s.n, 0), cap)) : 0) / 32;
@@ -340,8 +373,9 @@ __global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_fe
 #pragma unroll
         for (int pt = 0; pt < 2; ++pt) mask_scores(pos0 + pt * 16, qpos[qt], window, end, grp, sc[qt][pt]);
     }
+    softmax_scale(sc, c_log2, w, o);
 #pragma unroll
-    for (int qt = 0; qt < QT; ++qt) softmax_step(sc[qt], c_log2, w[qt], o[qt]);
+    for (int qt = 0; qt < QT; ++qt) softmax_weights(sc[qt], w[qt]);
     if (masked) {
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) clean_values(vf[dt], pos0, qpos, window, end, grp, o, dt);
@@ -417,7 +451,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedView c, PagedRows 
   __shared__ int words[2 * kMaxPagedB];
   Place pl;
   if (!find_place(c, r, window, k, true, blockIdx.x, words, words + kMaxPagedB, nullptr, &pl)) return;
-  const SeqRows s = seq_rows(c, r, pl.b);
+  const SeqRows s = uniform(seq_rows(c, r, pl.b));
   const int lane = threadIdx.x & 63;
   const size_t step = static_cast<size_t>(c.H) * k.tile;         // from range to range
   for (int in = blockIdx.y * 4 + (threadIdx.x >> 6); in < k.tile; in += 4 * gridDim.y) {
@@ -456,10 +490,10 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedView c, PagedRows 
 // these are computed. What bounds it is the matrix units (QT 64-cycle products
 // per KiB of LDS read) with the softmax's vector work beside them, which the
 // second wave of every SIMD covers.
-__device__ __forceinline__ void copy_to_lds(const void* src, uint32_t lds) {
+__device__ __forceinline__ void copy_to_lds(const void* src, uint32_t lane_offset, uint32_t lds) {
   // Untracked by the compiler's wait counts: it would make every LDS read wait
   // for the copies of the other stage too.
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(lds) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_offset), "s"(src), "{m0}"(lds) : "memory");
 }
 
 template <typename T, int DH, int QT, int NW>
@@ -478,21 +512,23 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
   int* words = reinterpret_cast<int*>(stage);
   Place pl;
   if (!find_place(c, r, window, k, false, blockIdx.x, words, words + kMaxPagedB, err, &pl)) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int r16 = lane & 15, grp = lane >> 4;
-  const SeqRows s = seq_rows(c, r, pl.b);
+  const SeqRows s = uniform(seq_rows(c, r, pl.b));
   const int cap = c.max_pages << c.page_log2;
   // The last tiles of a prompt see most: they go first.
-  const int nrows = s.n * c.G, ntiles = (nrows + k.tile - 1) / k.tile;
+  const int nrows = s.n * c.G, ntiles = uniform((nrows + k.tile - 1) / k.tile);
   const int tile = pl.ranges > 1 ? pl.tile : ntiles - 1 - pl.tile;
   const int row0 = tile * k.tile, wrow0 = row0 + wave * WR;
-  const int first = s.p0 + row0 / c.G, last = s.p0 + (min(row0 + k.tile, nrows) - 1) / c.G;
+  const int first = s.p0 + uniform(row0 / c.G), last = s.p0 + uniform((min(row0 + k.tile, nrows) - 1) / c.G);
   const int end = min(max(last + 1, 0), cap);
   const int lo = window ? min(max(first - window + 1, 0), end) : 0;
   const int base = (window ? min(max(s.p0 - window + 1, 0), min(max(s.p0 + s.n, 0), cap)) : 0) / 32;
-  const int blk0 = max(base + pl.range * pl.per, lo / 32), blk1 = min(base + (pl.range + 1) * pl.per, (end + 31) / 32);
+  const int blk0 = uniform(max(base + pl.range * pl.per, lo / 32));
+  const int blk1 = uniform(min(base + (pl.range + 1) * pl.per, (end + 31) / 32));
   // The same of this wave's rows; none: wlast < 0.
-  const int wfirst = s.p0 + wrow0 / c.G, wlast = wrow0 < nrows ? s.p0 + (min(wrow0 + WR, nrows) - 1) / c.G : -1;
+  const int wfirst = s.p0 + uniform(wrow0 / c.G);
+  const int wlast = wrow0 < nrows ? s.p0 + uniform((min(wrow0 + WR, nrows) - 1) / c.G) : -1;
   const float c_log2 = scale * 1.4426950408889634f;
 
   Frag<T> qf[QT][DH / 32];
@@ -532,91 +568,157 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
     }
     return __builtin_amdgcn_readlane(id, blk - id0);
   };
-  // Copy the blocks from blk on (up to NB) into stage b; bit h of the result: block h is there.
+  // Copy the blocks from blk on (up to NB) into stage b; bit h of the result:
+  // block h is there. A wave's share lies in one block's keys or values.
+  constexpr int kShare = 2 * NB * kCopies / NW;
+  static_assert(kCopies % kShare == 0, "one plane per wave");
+  const int share_h = wave * kShare / (2 * kCopies), share_kv = wave * kShare / kCopies & 1;
+  const char* plane = static_cast<const char*>(share_kv ? c.v : c.k) + wave * kShare % kCopies * 1024;
   auto fetch = [&](int blk, int b) {
     uint32_t there = 0;
-    size_t off[NB];
+    int mine = -1;
 #pragma unroll
     for (int h = 0; h < NB; ++h) {
       const int page = blk + h < blk1 ? page_of(blk + h) : -1;
-      off[h] = (static_cast<size_t>(max(page, 0)) * c.H + pl.kvh) * area + static_cast<size_t>((blk + h) * 32 & in_page) * DH;
       there |= page >= 0 ? 1u << h : 0;
+      if (h == share_h) mine = page;
     }
+    if (mine >= 0) {
+      const size_t off = (static_cast<size_t>(mine) * c.H + pl.kvh) * area + static_cast<size_t>((blk + share_h) * 32 & in_page) * DH;
+      const char* src = uniform(plane + off * sizeof(T));
+      const uint32_t dst = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&stage[b])) + wave * kShare * 1024;
 #pragma unroll
-    for (int j = 0; j < 2 * NB * kCopies / NW; ++j) {
-      const int n = wave * (2 * NB * kCopies / NW) + j;
-      const int h = n / (2 * kCopies), kv = n / kCopies & 1, at = n % kCopies;
-      if (!(there >> h & 1)) continue;
-      const char* src = static_cast<const char*>(kv ? c.v : c.k) + (h ? off[NB - 1] : off[0]) * sizeof(T) + at * 1024 + lane * 16;
-      copy_to_lds(src, static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&stage[b][h][kv][0])) + at * 1024);
+      for (int j = 0; j < kShare; ++j) copy_to_lds(src + j * 1024, lane * 16, dst + j * 1024);
     }
     return there;
   };
   __syncthreads();                                 // the plan's words have been read
-  uint32_t there = blk0 < blk1 ? fetch(blk0, 0) : 0;
-  int b = 0;
-  for (int blk = blk0; blk < blk1; blk += NB, b ^= 1) {
-    // This stage's copies have landed, and the other one's reads are over, in every wave.
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    const uint32_t next = blk + NB < blk1 ? fetch(blk + NB, b ^ 1) : 0;
-    const int pos0 = blk * 32;
-    uint32_t on = 0;                               // blocks this wave's rows see anything of
+  // A stage's scores: NH blocks from h0 on.
+  auto scores = [&](auto& sc, int b, int h0) {
+    constexpr int NT = sizeof(sc[0]) / sizeof(f32x4);
 #pragma unroll
-    for (int h = 0; h < NB; ++h)
-      on |= pos0 + h * 32 <= wlast && !(window && pos0 + h * 32 + 31 <= wfirst - window) ? there & 1u << h : 0;
-    there = next;
-    if (!on) continue;
-    const bool all = on == (1u << NB) - 1 && pos0 + NB * 32 - 1 <= min(wfirst, end - 1) && !(window && pos0 <= wlast - window);
-    // One straight run over the stage where every row sees all of it; else
-    // block by block.
-    auto step = [&](auto whole, int h0) {
-      constexpr bool kWhole = decltype(whole)::value;
-      constexpr int NH = kWhole ? NB : 1;
-      const T(*st)[2][kTile] = &stage[b][h0];
-      f32x4 sc[QT][2 * NH];
+    for (int pt = 0; pt < NT; ++pt) {
 #pragma unroll
-      for (int pt = 0; pt < 2 * NH; ++pt) {
+      for (int qt = 0; qt < QT; ++qt) sc[qt][pt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt) sc[qt][pt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int dt = 0; dt < DH / 32; ++dt) {
+        const Frag<T> kf = load_frag(&stage[b][h0 + (pt >> 1)][0][(((pt & 1) * (DH / 32) + dt) * 64 + lane) * 8]);
 #pragma unroll
-        for (int dt = 0; dt < DH / 32; ++dt) {
-          const Frag<T> kf = load_frag(&st[pt >> 1][0][(((pt & 1) * (DH / 32) + dt) * 64 + lane) * 8]);
-#pragma unroll
-          for (int qt = 0; qt < QT; ++qt) sc[qt][pt] = mma8(sc[qt][pt], kf, qf[qt][dt]);
-        }
-        if (!kWhole) {
-#pragma unroll
-          for (int qt = 0; qt < QT; ++qt) mask_scores(pos0 + (h0 * 2 + pt) * 16, qpos[qt], window, end, grp, sc[qt][pt]);
-        }
+        for (int qt = 0; qt < QT; ++qt) sc[qt][pt] = mma8(sc[qt][pt], kf, qf[qt][dt]);
       }
+    }
+  };
+  // Weights rounded once to the type (bf16: half a step, 2^-8 of each, which
+  // averages out over a row like the values' own rounding; a second product
+  // of what is left off would cost half as much again).
+  auto rounded = [&](const f32x4& x, const f32x4& y) {
+    Frag<T> f;
 #pragma unroll
-      for (int qt = 0; qt < QT; ++qt) softmax_step(sc[qt], c_log2, w[qt], o[qt]);
-      // Weights rounded once to the type (bf16: half a step, 2^-8 of each, which
-      // averages out over a row like the values' own rounding; a second product
-      // of what is left off would cost half as much again).
+    for (int e = 0; e < 4; ++e) {
+      f.v[e] = from_f32<T>(x[e]);
+      f.v[4 + e] = from_f32<T>(y[e]);
+    }
+    return f;
+  };
+  uint32_t there = blk0 < blk1 ? fetch(blk0, 0) : 0, next = 0, on = 0;
+  bool ready = false;
+  int b = 0, blk = blk0;
+  while (blk < blk1) {
+    // Stages that every row of the wave sees all of, and whose scores need no
+    // new reference: one straight run, with nothing but products on the
+    // accumulators (other paths through it cost their copies).
+    while (true) {
+      const int pos0 = blk * 32;
+      if (!ready) {
+        // This stage's copies have landed, and the other one's reads are over, in every wave.
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        next = blk + NB < blk1 ? fetch(blk + NB, b ^ 1) : 0;
+        on = 0;                                    // blocks this wave's rows see anything of
 #pragma unroll
-      for (int h = 0; h < NH; ++h) {
+        for (int h = 0; h < NB; ++h)
+          on |= pos0 + h * 32 <= wlast && !(window && pos0 + h * 32 + 31 <= wfirst - window) ? there & 1u << h : 0;
+        ready = true;
+      }
+      if (on != (1u << NB) - 1 || pos0 + NB * 32 - 1 > min(wfirst, end - 1) || (window && pos0 <= wlast - window)) break;
+      f32x4 sc[QT][2 * NB];
+      scores(sc, b, 0);
+      bool up = false;
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) up |= scale_scores(sc[qt], c_log2, w[qt]) > w[qt].lim;
+      // Key fragments are read four ahead of their products.
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int g = 0; g < 2 * NB * (DH / 32) - 4; ++g) {
+        __builtin_amdgcn_sched_group_barrier(0x008, QT, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 4 * QT, 0);
+      if (__ballot(up)) break;
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) softmax_weights(sc[qt], w[qt]);
+#pragma unroll
+      for (int h = 0; h < NB; ++h) {
         Frag<T> pf[QT];
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) pf[qt].v[e] = from_f32<T>(sc[qt][h * 2 + (e >> 2)][e & 3]);
+        for (int qt = 0; qt < QT; ++qt) pf[qt] = rounded(sc[qt][2 * h], sc[qt][2 * h + 1]);
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) {
-          Frag<T> vf = load_frag(&st[h][1][(dt * 64 + lane) * 8]);
-          if (!kWhole) clean_values(vf, pos0 + h0 * 32, qpos, window, end, grp, o, dt);
+          const Frag<T> vf = load_frag(&stage[b][h][1][(dt * 64 + lane) * 8]);
 #pragma unroll
           for (int qt = 0; qt < QT; ++qt) o[qt][dt] = mma8(o[qt][dt], vf, pf[qt]);
         }
       }
-    };
-    if (all) {
-      step(std::true_type{}, 0);
-    } else {
-#pragma unroll 1
-      for (int h = 0; h < NB; ++h)
-        if (on >> h & 1) step(std::false_type{}, h);
+      ready = false;
+      there = next;
+      b ^= 1;
+      blk += NB;
+      if (blk >= blk1) break;
     }
+    if (blk >= blk1) break;
+    // The others block by block.
+#pragma unroll 1
+    for (int h = 0; h < NB; ++h) {
+      if (!(on >> h & 1)) continue;
+      const int pos0 = (blk + h) * 32;
+      f32x4 sc[QT][2];
+      scores(sc, b, h);
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+        for (int pt = 0; pt < 2; ++pt) mask_scores(pos0 + pt * 16, qpos[qt], window, end, grp, sc[qt][pt]);
+      softmax_scale(sc, c_log2, w, o);
+      Frag<T> pf[QT];
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) {
+        softmax_weights(sc[qt], w[qt]);
+        pf[qt] = rounded(sc[qt][0], sc[qt][1]);
+      }
+      // The values times zero: NaN if one of them is not finite.
+      f32x4 zero{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt)
+        zero = mma8(zero, load_frag(&stage[b][h][1][(dt * 64 + lane) * 8]), Frag<T>::zero());
+      if (__ballot(zero[0] + zero[1] + zero[2] + zero[3] != 0.f) || pos0 + 32 > end) {
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) {
+          Frag<T> vf = load_frag(&stage[b][h][1][(dt * 64 + lane) * 8]);
+          clean_values(vf, pos0, qpos, window, end, grp, o, dt);
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt) o[qt][dt] = mma8(o[qt][dt], vf, pf[qt]);
+        }
+      } else {
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) {
+          const Frag<T> vf = load_frag(&stage[b][h][1][(dt * 64 + lane) * 8]);
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt) o[qt][dt] = mma8(o[qt][dt], vf, pf[qt]);
+        }
+      }
+    }
+    ready = false;
+    there = next;
+    b ^= 1;
+    blk += NB;
   }
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {

@@ -200,7 +200,7 @@ sps_status check_paged_rows(const sps_paged_config& c, bool ragged, int rows, in
 // positions, qt 16-row tiles each), those with more the other (their waves
 // take different rows).
 constexpr int kPagedMinBlocks = 8;     // 256 positions
-constexpr int kManyWaves = 8, kManyQt = 2;
+constexpr int kManyWaves = 4, kManyQt = 2;
 struct PagedClass {
   int tile, target;
   long items, slots, joins;            // the most there can be; items 0: no such sequence
