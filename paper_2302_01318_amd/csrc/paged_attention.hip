@@ -8,7 +8,7 @@
 // order is made for): both tiles go from the page straight into registers, a
 // KiB per wave and load. The waves' (O, max, sum) meet in LDS; ranges of one
 // tile meet in a second launch.
-#include <type_traits>
+#include <algorithm>
 
 #include "paged.h"
 
@@ -28,71 +28,157 @@ __device__ __forceinline__ SeqRows uniform(SeqRows s) {
   return s;
 }
 
-// Where an item, or a (tile, KV head) with several ranges, belongs.
+// Where an item belongs.
 struct Place {
+  SeqRows s;
   int b, tile, range, ranges, kvh;
   int per;                 // blocks per range
-  long slot;               // of the tile's first range (ranges > 1)
+  long slot;               // of the tile's first range (ranges > 1); the others follow H apart
 };
 
 // Sequences with more than `above` and up to `limit` query rows, in tiles of
-// `tile` (plan.h).
+// `tile` (plan.h). split: the cost of an item's partials in blocks.
 struct Class {
-  int tile, target, above, limit;
+  int tile, target, above, limit, split;
 };
 
-// The tiles and blocks of every sequence of the class, per sequence in LDS,
-// and from them the place of item (join: of the (tile, KV head) pair) number
-// `idx`. Every work-group of both launches computes the same plan from the
-// same lengths. Returns false past the last one.
-__device__ __forceinline__ bool find_place(const PagedView& c, const PagedRows& r, int window, const Class& k,
-                                           bool join, uint32_t idx, int* s_tiles, int* s_blocks, int* err, Place* out) {
-  const int lane = threadIdx.x & 63;
+// What the second launch has to join: entry i of the slots' descriptors, if i
+// is a tile's first slot (ranges > 1).
+struct Join {
+  int r0, rows, tile, kvh, ranges;
+};
+
+// A sequence's tiles in the class, and the blocks that its rows see.
+__device__ __forceinline__ int2 tiles_blocks(const PagedView& c, const Class& k, const SeqRows& s, int window) {
   const int cap = c.max_pages << c.page_log2;
-  for (int b = threadIdx.x; b < c.B; b += blockDim.x) {
-    const SeqRows s = seq_rows(c, r, b);
-    if (s.bad && idx == 0 && err) atomicOr(err, kErrCapacity);
-    const int end = min(max(s.p0 + s.n, 0), cap);
-    const int lo = window ? min(max(s.p0 - window + 1, 0), end) : 0;
-    const int rows = s.n * c.G;
-    s_tiles[b] = rows > k.above && rows <= k.limit ? (rows + k.tile - 1) / k.tile : 0;
-    s_blocks[b] = (end + 31) / 32 - lo / 32;
+  const int end = min(max(s.p0 + s.n, 0), cap);
+  const int lo = window ? min(max(s.p0 - window + 1, 0), end) : 0;
+  const int rows = s.n * c.G;
+  return make_int2(rows > k.above && rows <= k.limit ? static_cast<int>((rows + k.tile - 1u) / k.tile) : 0,
+                   (end + 31) / 32 - lo / 32);
+}
+
+// Blocks per range, by up to 64 sequences' tiles and blocks (one a lane): lane
+// r - 1 prices r ranges of the longest, in the time of a block: the rounds that
+// the items take over the card's `target` slots, or where sizes or rounds are
+// uneven the work per slot and most of an item until the last one ends
+// (work-groups go faster as others end). An item costs kItemBlocks beside its
+// blocks, one of several ranges k.split more for its partials, and the joining
+// kJoinBlocks. Every lane takes the cheapest.
+constexpr int kItemBlocks = 4, kJoinBlocks = 3;
+__device__ __forceinline__ int blocks_per_range(const PagedView& c, const Class& k, int tiles, int blocks) {
+  const int lane = threadIdx.x & 63;
+  int most = 0;
+  for (int b = 0; b < c.B; ++b) most = max(most, __builtin_amdgcn_readlane(blocks, b));
+  const int per = max(kPagedMinBlocks, static_cast<int>((most + lane) / (lane + 1u)));
+  const float inv = 1.f / per;
+  int items = 0;
+  float work = 0.f;
+  for (int b = 0; b < c.B; ++b) {
+    const int t = __builtin_amdgcn_readlane(tiles, b), n = __builtin_amdgcn_readlane(blocks, b) + per - 1;
+    int ranges = static_cast<int>(n * inv);        // n / per: at most one off
+    ranges += (ranges + 1) * per <= n ? 1 : ranges * per > n ? -1 : 0;
+    items += t * max(ranges, 1);
+    work += static_cast<float>(t) * (n - per + 1);
   }
-  __syncthreads();
-  uint64_t all = 0;
-  for (int b0 = 0; b0 < c.B; b0 += 64)
-    all += wave_sum_u64(b0 + lane < c.B ? static_cast<uint64_t>(s_tiles[b0 + lane]) * s_blocks[b0 + lane] : 0);
-  const int per = uniform(max(kPagedMinBlocks, static_cast<int>(ceil(static_cast<double>(all) * c.H / k.target))));
-  const int want = uniform(static_cast<int>(idx) / c.H), h = static_cast<int>(idx) - want * c.H;
-  uint64_t before = 0;                             // (items or joins) << 32 | slots, per KV head
-  for (int b0 = 0; b0 < c.B; b0 += 64) {
-    const int b = b0 + lane;
-    const uint32_t tiles = b < c.B ? s_tiles[b] : 0;
-    const uint32_t ranges = b < c.B ? max(1, (s_blocks[b] + per - 1) / per) : 1;
-    const uint32_t slots = ranges > 1 ? tiles * ranges : 0;
-    const uint32_t mine = join ? (ranges > 1 ? tiles : 0) : tiles * ranges;
-    const uint64_t incl = wave_incl_scan_u64(static_cast<uint64_t>(mine) << 32 | slots) + before;
-    const uint64_t hit = __ballot(want < static_cast<int>(incl >> 32));
-    if (hit) {
-      const int src = __ffsll(static_cast<unsigned long long>(hit)) - 1;
-      const uint64_t inc = readlane_u64(incl, src);
-      const int m = __builtin_amdgcn_readlane(static_cast<int>(mine), src);
-      const int sl = __builtin_amdgcn_readlane(static_cast<int>(slots), src);
-      const int nr = __builtin_amdgcn_readlane(static_cast<int>(ranges), src);
-      const int at = static_cast<int>(want - (static_cast<int>(inc >> 32) - m));
-      out->b = uniform(b0 + src);
-      out->ranges = nr;
-      out->tile = join ? at : uniform(at / nr);
-      out->range = join ? 0 : at - out->tile * nr;
-      out->kvh = h;
-      out->per = per;
-      const uint32_t slot0 = static_cast<uint32_t>(inc) - sl;
-      out->slot = (static_cast<long>(slot0) + static_cast<long>(out->tile) * nr) * c.H + h;   // ranges H apart
-      return true;
+  const bool split = lane && per < most;
+  const float own = static_cast<float>(kItemBlocks + (split ? k.split : 0));
+  const float n = static_cast<float>(items) * c.H, slots = static_cast<float>(k.target);
+  const float each = min(per, most) + own;
+  float cost = fminf(ceilf(n / slots) * each, (work * c.H + n * own) / fminf(n, slots) + 0.75f * each);
+  if (split) cost += kJoinBlocks;
+  if (lane && n > kPagedMostItems * slots) cost = INFINITY;        // the workspace's bound
+  float best = cost;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) best = fminf(best, __shfl_xor(best, o));
+  const uint64_t cheapest = __ballot(cost == best);
+  return cheapest ? __builtin_amdgcn_readlane(per, __ffsll(static_cast<unsigned long long>(cheapest)) - 1) : kPagedMinBlocks;
+}
+
+// One step of the search for item `want` (of H KV heads each): `tiles` and
+// `blocks` of 64 sequences, one a lane; *before: (items << 32 | slots) of the
+// sequences before them. The lane that has it, or -1.
+__device__ __forceinline__ int find_lane(int tiles, int blocks, int per, int want, int kvh, int H, uint64_t* before,
+                                         Place* out) {
+  const uint32_t ranges = max(1u, (blocks + per - 1u) / per);
+  const uint32_t slots = ranges > 1 ? tiles * ranges : 0, mine = tiles * ranges;
+  const uint64_t incl = wave_incl_scan_u64(static_cast<uint64_t>(mine) << 32 | slots) + *before;
+  const uint64_t hit = __ballot(want < static_cast<int>(incl >> 32));
+  *before = readlane_u64(incl, 63);
+  if (!hit) return -1;
+  const int src = __ffsll(static_cast<unsigned long long>(hit)) - 1;
+  const uint64_t inc = readlane_u64(incl, src);
+  const int at = want - (static_cast<int>(inc >> 32) - __builtin_amdgcn_readlane(static_cast<int>(mine), src));
+  out->ranges = __builtin_amdgcn_readlane(static_cast<int>(ranges), src);
+  out->tile = uniform(static_cast<int>(static_cast<uint32_t>(at) / static_cast<uint32_t>(out->ranges)));
+  out->range = at - out->tile * out->ranges;
+  out->kvh = kvh;
+  out->per = per;
+  const uint32_t slot0 = static_cast<uint32_t>(inc) - __builtin_amdgcn_readlane(static_cast<int>(slots), src);
+  out->slot = (static_cast<long>(slot0) + static_cast<long>(out->tile) * out->ranges) * H + kvh;
+  return src;
+}
+
+// The place of item number blockIdx.x; false past the last. Every work-group
+// computes the same plan from the same lengths; the first one leaves the number
+// of slots in *count. `words`: LDS for 2 kMaxPagedB ints, free again after the next barrier.
+__device__ __forceinline__ bool find_place(const PagedView& c, const PagedRows& r, int window, const Class& k, int* words,
+                                           int* count, int* err, Place* out) {
+  const int lane = threadIdx.x & 63, idx = blockIdx.x;
+  const int want = uniform(static_cast<int>(static_cast<uint32_t>(idx) / static_cast<uint32_t>(c.H)));
+  const int kvh = idx - want * c.H;
+  uint64_t before = 0;
+  bool found = false;
+  if (c.B <= 64) {
+    // A sequence a lane, in registers.
+    SeqRows s{};
+    if (lane < c.B) s = seq_rows(c, r, lane);
+    if (idx == 0 && s.bad) atomicOr(err, kErrCapacity);
+    const int2 tb = lane < c.B ? tiles_blocks(c, k, s, window) : make_int2(0, 0);
+    const int per = blocks_per_range(c, k, tb.x, tb.x ? tb.y : 0);
+    const int src = find_lane(tb.x, tb.y, per, want, kvh, c.H, &before, out);
+    if (src >= 0) {
+      out->b = src;
+      out->s.r0 = __builtin_amdgcn_readlane(s.r0, src);
+      out->s.n = __builtin_amdgcn_readlane(s.n, src);
+      out->s.p0 = __builtin_amdgcn_readlane(s.p0, src);
+      found = true;
     }
-    before = readlane_u64(incl, 63);
+  } else {
+    // More sequences fill the card by themselves: about `target` items and one per tile.
+    int *s_tiles = words, *s_blocks = words + kMaxPagedB;
+    for (int b = threadIdx.x; b < c.B; b += blockDim.x) {
+      const SeqRows s = seq_rows(c, r, b);
+      if (idx == 0 && s.bad) atomicOr(err, kErrCapacity);
+      const int2 tb = tiles_blocks(c, k, s, window);
+      s_tiles[b] = tb.x;
+      s_blocks[b] = tb.y;
+    }
+    __syncthreads();
+    uint64_t all = 0;
+    for (int b0 = 0; b0 < c.B; b0 += 64)
+      all += wave_sum_u64(b0 + lane < c.B ? static_cast<uint64_t>(s_tiles[b0 + lane]) * s_blocks[b0 + lane] : 0);
+    const int per = uniform(max(kPagedMinBlocks, static_cast<int>(ceil(static_cast<double>(all) * c.H / k.target))));
+    for (int b0 = 0; b0 < c.B && (!found || idx == 0); b0 += 64) {
+      Place here;
+      const int b = b0 + lane;
+      const int src = find_lane(b < c.B ? s_tiles[b] : 0, b < c.B ? s_blocks[b] : 0, per, want, kvh, c.H, &before, &here);
+      if (src < 0 || found) continue;
+      *out = here;
+      out->b = uniform(b0 + src);
+      out->s = uniform(seq_rows(c, r, out->b));
+      found = true;
+    }
   }
-  return false;
+  if (idx == 0 && threadIdx.x == 0) *count = static_cast<int>(static_cast<uint32_t>(before)) * c.H;
+  return found;
+}
+
+// A tile's first range leaves what the second launch needs, the others that there is nothing.
+__device__ __forceinline__ void leave_join(const PagedView& c, const Place& pl, Join* joins) {
+  if (threadIdx.x == 0 && pl.ranges > 1)
+    joins[pl.slot + static_cast<long>(pl.range) * c.H] =
+        Join{pl.s.r0, pl.s.n * c.G, pl.tile, pl.kvh, pl.range == 0 ? pl.ranges : 0};
 }
 
 template <typename T> __device__ __forceinline__ bool nonfinite(T x);
@@ -249,27 +335,23 @@ __device__ __forceinline__ void write_row(const PagedView& c, const Class& k, co
     lse[static_cast<size_t>(tok) * c.H * c.G + head] = l == 0.f ? -INFINITY : 0.69314718f * ref + logf(l);
 }
 
-constexpr int decode_waves(int es, int DH, int QT) {
-  const int regs = DH * es / 4 + DH * QT * 3 / 8 * (es == 4 ? 4 : 3) / 3 + 90;
-  return regs <= 168 ? 3 : regs <= 256 ? 2 : 1;
-}
 template <typename T, int DH, int QT>
-__global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_few_kernel(PagedView c, PagedRows r, Class k,
+__global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedView c, PagedRows r, Class k,
                                                          const T* __restrict__ q, int64_t ldq, float scale, int window,
                                                          T* __restrict__ out, int64_t ldo, float* __restrict__ lse,
                                                          float* __restrict__ part_o, float2* __restrict__ part_ml,
-                                                         int* err) {
+                                                         Join* __restrict__ joins, int* __restrict__ count, int* err) {
   constexpr int TR = 16 * QT, ND = DH / 16;
   // The plan's words per sequence, then two waves' (O, max, sum).
   constexpr int kMergeF4 = 2 * QT * ND * 64, kPlanF4 = 2 * kMaxPagedB / 4;
   __shared__ f32x4 sm[kMergeF4 > kPlanF4 ? kMergeF4 : kPlanF4];
   __shared__ float2 sml[2 * QT * 64];
-  int* s_tiles = reinterpret_cast<int*>(sm);
   Place pl;
-  if (!find_place(c, r, window, k, false, blockIdx.x, s_tiles, s_tiles + kMaxPagedB, err, &pl)) return;
+  if (!find_place(c, r, window, k, reinterpret_cast<int*>(sm), count, err, &pl)) return;
+  leave_join(c, pl, joins);
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int r16 = lane & 15, grp = lane >> 4;
-  const SeqRows s = uniform(seq_rows(c, r, pl.b));
+  const SeqRows& s = pl.s;
   const int cap = c.max_pages << c.page_log2;
   const int nrows = s.n * c.G, row0 = pl.tile * TR;
   // Positions of the tile's first and last token, and what they see.
@@ -280,7 +362,11 @@ __global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_fe
   const int blk0 = max(base + pl.range * pl.per, lo / 32), blk1 = min(base + (pl.range + 1) * pl.per, (end + 31) / 32);
   const float c_log2 = scale * 1.4426950408889634f;
 
-  Frag<T> qf[QT][DH / 32];
+  // The queries' fragments, in registers or (kStaged: more than a 16-row tile,
+  // or fp32) in LDS, where all waves read them: two waves per SIMD need the room.
+  constexpr bool kStaged = QT > 1 || sizeof(T) == 4;
+  __shared__ Frag<T> sq[kStaged ? QT * (DH / 32) * 64 : 1];
+  Frag<T> qf[kStaged ? 1 : DH / 32];
   int qpos[QT], tok[QT], head[QT];
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {
@@ -291,9 +377,15 @@ __global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_fe
     head[qt] = pl.kvh * c.G + (valid ? row - t * c.G : 0);
     qpos[qt] = valid ? s.p0 + t : -1;
 #pragma unroll
-    for (int dt = 0; dt < DH / 32; ++dt)
-      qf[qt][dt] = valid ? load_frag_any(q + tok[qt] * ldq + head[qt] * DH + dt * 32 + grp * 8) : Frag<T>::zero();
+    for (int dt = 0; dt < DH / 32; ++dt) {
+      const T* src = q + tok[qt] * ldq + head[qt] * DH + dt * 32 + grp * 8;
+      if (!kStaged)
+        qf[dt] = valid ? load_frag_any(src) : Frag<T>::zero();
+      else if ((qt * (DH / 32) + dt) % 4 == wave)
+        sq[(qt * (DH / 32) + dt) * 64 + lane] = valid ? load_frag_any(src) : Frag<T>::zero();
+    }
   }
+  auto query = [&](int qt, int dt) { return kStaged ? sq[(qt * (DH / 32) + dt) * 64 + lane] : qf[kStaged ? 0 : dt]; };
   RowSoftmax w[QT];
   f32x4 o[QT][ND];
 #pragma unroll
@@ -348,40 +440,28 @@ __global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_fe
     for (int dt = 0; dt < ND; ++dt) vf[dt] = load_frag_stream(vp + dt * 512);
   };
   pages(0);
+  __syncthreads();                                 // the staged queries; the plan's words have been read
   int i = seek(0);
   if (i < nb) {
     load_keys();
     load_values();
   }
-  while (i < nb) {
-    const int pos0 = (blk0 + wave + 4 * i) * 32;
-    f32x4 sc[QT][2];
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt)
-#pragma unroll
-      for (int pt = 0; pt < 2; ++pt) {
-        sc[qt][pt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int dt = 0; dt < DH / 32; ++dt) sc[qt][pt] = mma8(sc[qt][pt], kf[pt][dt], qf[qt][dt]);
-      }
-    const int next = seek(i + 1);
-    if (next < nb) load_keys();
-    const bool masked = pos0 + 31 > first || pos0 + 31 >= end || (window && pos0 <= last - window);
-    if (masked) {
-#pragma unroll
-      for (int qt = 0; qt < QT; ++qt)
-#pragma unroll
-        for (int pt = 0; pt < 2; ++pt) mask_scores(pos0 + pt * 16, qpos[qt], window, end, grp, sc[qt][pt]);
-    }
-    softmax_scale(sc, c_log2, w, o);
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) softmax_weights(sc[qt], w[qt]);
-    if (masked) {
-#pragma unroll
-      for (int dt = 0; dt < ND; ++dt) clean_values(vf[dt], pos0, qpos, window, end, grp, o, dt);
-    }
+  auto scores = [&](f32x4 (&sc)[QT][2]) {
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
+      sc[qt][0] = sc[qt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int dt = 0; dt < DH / 32; ++dt) {
+        const Frag<T> qd = query(qt, dt);
+#pragma unroll
+        for (int pt = 0; pt < 2; ++pt) sc[qt][pt] = mma8(sc[qt][pt], kf[pt][dt], qd);
+      }
+    }
+  };
+  auto products = [&](f32x4 (&sc)[QT][2]) {
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      softmax_weights(sc[qt], w[qt]);
       // bf16: the weights as hi + lo, p to 2^-16 relative; the second product
       // costs nothing where the loads are what takes the time.
       Frag<T> hi, lw;
@@ -397,8 +477,47 @@ __global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_fe
         if (sizeof(T) == 2) o[qt][dt] = mma8(o[qt][dt], vf[dt], lw);
       }
     }
-    if (next < nb) load_values();
-    i = next;
+  };
+  while (i < nb) {
+    f32x4 sc[QT][2];
+    // Blocks that every row sees all of and that need no new reference: nothing
+    // but products on the accumulators.
+    while (true) {
+      const int pos0 = (blk0 + wave + 4 * i) * 32;
+      if (pos0 + 31 > min(first, end - 1) || (window && pos0 <= last - window)) break;
+      scores(sc);
+      bool up = false;
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) up |= scale_scores(sc[qt], c_log2, w[qt]) > w[qt].lim;
+      if (__ballot(up)) break;
+      const int next = seek(i + 1);
+      if (next < nb) load_keys();
+      products(sc);
+      if (next < nb) load_values();
+      i = next;
+      if (i >= nb) break;
+    }
+    if (i >= nb) break;
+    const int pos0 = (blk0 + wave + 4 * i) * 32;
+    scores(sc);
+    const bool masked = pos0 + 31 > min(first, end - 1) || (window && pos0 <= last - window);
+    if (masked) {
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+        for (int pt = 0; pt < 2; ++pt) mask_scores(pos0 + pt * 16, qpos[qt], window, end, grp, sc[qt][pt]);
+    }
+    softmax_scale(sc, c_log2, w, o);
+    if (masked) {
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) clean_values(vf[dt], pos0, qpos, window, end, grp, o, dt);
+    }
+    products(sc);
+    i = seek(i + 1);
+    if (i < nb) {
+      load_keys();
+      load_values();
+    }
   }
 
   // Waves 2, 3 into 0, 1, then 1 into 0.
@@ -409,7 +528,6 @@ __global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_fe
     sum[qt] = w[qt].sum + __shfl_xor(w[qt].sum, 16);
     sum[qt] += __shfl_xor(sum[qt], 32);
   }
-  __syncthreads();                                 // the plan's words have been read
 #pragma unroll
   for (int half = 2; half; half >>= 1) {
     if (wave >= half && wave < 2 * half) {
@@ -443,44 +561,46 @@ __global__ __launch_bounds__(256, decode_waves(sizeof(T), DH, QT)) void paged_fe
                        part_ml);
 }
 
-// The ranges of a tile's rows joined: one wave per row.
+// The ranges of a tile's rows joined: 16 lanes per row, four rows per wave (one
+// row's loads wait for each other, so rows in flight are what counts).
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedView c, PagedRows r, Class k, int window, const float* __restrict__ part_o,
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedView c, int tile_rows, const Join* __restrict__ joins,
+                                                         const int* __restrict__ count, const float* __restrict__ part_o,
                                                          const float2* __restrict__ part_ml, T* __restrict__ out,
                                                          int64_t ldo, float* __restrict__ lse) {
-  __shared__ int words[2 * kMaxPagedB];
-  Place pl;
-  if (!find_place(c, r, window, k, true, blockIdx.x, words, words + kMaxPagedB, nullptr, &pl)) return;
-  const SeqRows s = uniform(seq_rows(c, r, pl.b));
-  const int lane = threadIdx.x & 63;
-  const size_t step = static_cast<size_t>(c.H) * k.tile;         // from range to range
-  for (int in = blockIdx.y * 4 + (threadIdx.x >> 6); in < k.tile; in += 4 * gridDim.y) {
-    const int row = pl.tile * k.tile + in;
-    if (row >= s.n * c.G) return;
-    const float2* ml = part_ml + pl.slot * k.tile + in;
-    const float* po = part_o + (pl.slot * k.tile + in) * DH + lane * (DH / 64);
-    float m = -INFINITY;
-    for (int i = lane; i < pl.ranges; i += 64) m = fmaxf(m, ml[i * step].x);
-    m = wave_max(m);
-    float l = 0.f, acc[DH / 64] = {};
-    if (m != -INFINITY) {
-#pragma unroll 8
-      for (int i = 0; i < pl.ranges; ++i) {
-        const float2 x = ml[i * step];
-        if (x.x == -INFINITY) continue;
-        const float w = fast_exp2(x.x - m);
-        l += w * x.y;
+  constexpr int NV = DH / 64;                      // 4-dim pieces per lane
+  const long slot = blockIdx.x;
+  const Join j = joins[slot];                      // inside the workspace, written if below the count
+  if (slot >= *count || j.ranges == 0) return;
+  const int in = blockIdx.y * 16 + static_cast<int>(threadIdx.x >> 4), lane = threadIdx.x & 15;
+  const int row = j.tile * tile_rows + in;
+  if (row >= j.rows) return;                       // tile_rows is a multiple of 16
+  const size_t step = static_cast<size_t>(c.H) * tile_rows;      // from range to range
+  const float2* ml = part_ml + slot * tile_rows + in;
+  const float* po = part_o + (slot * tile_rows + in) * DH + lane * 4;
+  float m = -INFINITY;
+  for (int i = lane; i < j.ranges; i += 16) m = fmaxf(m, ml[i * step].x);
 #pragma unroll
-        for (int d = 0; d < DH / 64; ++d) acc[d] += w * po[i * step * DH + d];
-      }
-    }
-    const int t = row / c.G, tok = s.r0 + t, head = pl.kvh * c.G + row - t * c.G;
+  for (int o = 1; o < 16; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+  const float mu = m == -INFINITY ? 0.f : m;
+  float l = 0.f;
+  f32x4 acc[NV] = {};
+#pragma unroll 4
+  for (int i = 0; i < j.ranges; ++i) {
+    const float2 x = ml[i * step];
+    const float wt = fast_exp2(x.x - mu);          // 0 for a range of which the row sees nothing (its partial is zero)
+    l += wt * x.y;
 #pragma unroll
-    for (int d = 0; d < DH / 64; ++d)
-      out[tok * ldo + head * DH + lane * (DH / 64) + d] = from_f32<T>(l == 0.f ? 0.f : acc[d] / l);
-    if (lse && lane == 0)
-      lse[static_cast<size_t>(tok) * c.H * c.G + head] = l == 0.f ? -INFINITY : 0.69314718f * m + logf(l);
+    for (int v = 0; v < NV; ++v) acc[v] += wt * *reinterpret_cast<const f32x4*>(po + i * step * DH + v * 64);
   }
+  const int t = static_cast<int>(static_cast<uint32_t>(row) / static_cast<uint32_t>(c.G));
+  const int tok = j.r0 + t, head = j.kvh * c.G + row - t * c.G;
+  const float inv = 1.f / l;
+#pragma unroll
+  for (int v = 0; v < NV; ++v)
+    store4_any(out + tok * ldo + head * DH + v * 64 + lane * 4, l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[v] * inv);
+  if (lse && lane == 0)
+    lse[static_cast<size_t>(tok) * c.H * c.G + head] = l == 0.f ? -INFINITY : 0.69314718f * m + logf(l);
 }
 
 // Sequences with many query rows: NW waves of 16 QT rows each against the
@@ -501,7 +621,8 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
                                                                 const T* __restrict__ q, int64_t ldq, float scale,
                                                                 int window, T* __restrict__ out, int64_t ldo,
                                                                 float* __restrict__ lse, float* __restrict__ part_o,
-                                                                float2* __restrict__ part_ml, int* err) {
+                                                                float2* __restrict__ part_ml, Join* __restrict__ joins,
+                                                                int* __restrict__ count, int* err) {
   constexpr int ND = DH / 16, WR = 16 * QT;
   constexpr int NB = sizeof(T) == 2 ? 2 : 1;                       // blocks per stage
   constexpr int kTile = 32 * DH;                                   // elements of a block's keys or values
@@ -509,12 +630,12 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
   static_assert(2 * NB * kCopies % NW == 0, "whole copies per wave");
   __shared__ __align__(1024) T stage[2][NB][2][kTile];
   static_assert(sizeof(stage) >= 2 * kMaxPagedB * sizeof(int), "the plan's words");
-  int* words = reinterpret_cast<int*>(stage);
   Place pl;
-  if (!find_place(c, r, window, k, false, blockIdx.x, words, words + kMaxPagedB, err, &pl)) return;
+  if (!find_place(c, r, window, k, reinterpret_cast<int*>(stage), count, err, &pl)) return;
+  leave_join(c, pl, joins);
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int r16 = lane & 15, grp = lane >> 4;
-  const SeqRows s = uniform(seq_rows(c, r, pl.b));
+  const SeqRows& s = pl.s;
   const int cap = c.max_pages << c.page_log2;
   // The last tiles of a prompt see most: they go first.
   const int nrows = s.n * c.G, ntiles = uniform((nrows + k.tile - 1) / k.tile);
@@ -733,39 +854,46 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
   }
 }
 
+// Three tiles are for bf16 alone (paged_few_tiles).
+template <typename T, int DH>
+static auto few_kernel_3() {
+  if constexpr (sizeof(T) == 2) return paged_few_kernel<T, DH, 3>;
+  else return paged_few_kernel<T, DH, 2>;
+}
+
+static_assert(sizeof(Join) == kPagedJoinBytes, "the workspace's entries");
+
 template <typename T, int DH>
 static hipError_t attn_t(const PagedView& c, const PagedRows& r, const PagedPlan& p, const void* q, int64_t ldq,
                          float scale, int window, void* out, int64_t ldo, float* lse, char* ws, int* err,
                          hipStream_t st) {
   const T* qq = static_cast<const T*>(q);
   T* oo = static_cast<T*>(out);
-  const Class few{p.few.tile, p.few.target, 0, p.limit}, many{p.many.tile, p.many.target, p.limit, INT32_MAX};
-  float *fo = reinterpret_cast<float*>(ws + p.few.o_off), *mo = reinterpret_cast<float*>(ws + p.many.o_off);
-  float2 *fm = reinterpret_cast<float2*>(ws + p.few.ml_off), *mm = reinterpret_cast<float2*>(ws + p.many.ml_off);
+  const Class few{p.few.tile, p.few.target, 0, p.limit, p.qt}, many{p.many.tile, p.many.target, p.limit, INT32_MAX, 16};
+  auto at = [&](size_t off) { return ws + off; };
   hipError_t e = hipSuccess;
   if (p.many.items) {
     hipLaunchKernelGGL((paged_many_kernel<T, DH, kManyQt, kManyWaves>), dim3(static_cast<unsigned>(p.many.items)),
-                       dim3(64 * kManyWaves), 0, st, c, r, many, qq, ldq, scale, window, oo, ldo, lse, mo, mm, err);
+                       dim3(64 * kManyWaves), 0, st, c, r, many, qq, ldq, scale, window, oo, ldo, lse,
+                       reinterpret_cast<float*>(at(p.many.o_off)), reinterpret_cast<float2*>(at(p.many.ml_off)),
+                       reinterpret_cast<Join*>(at(p.many.join_off)), reinterpret_cast<int*>(at(p.many.count_off)), err);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (p.few.items) {
-    auto kern = p.qt == 1   ? paged_few_kernel<T, DH, 1>
-                : p.qt == 2 ? paged_few_kernel<T, DH, 2>
-                : p.qt == 3 ? paged_few_kernel<T, DH, 3>
-                            : paged_few_kernel<T, DH, 4>;
+    auto kern = p.qt == 1 ? paged_few_kernel<T, DH, 1> : p.qt == 2 ? paged_few_kernel<T, DH, 2> : few_kernel_3<T, DH>();
     hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(p.few.items)), dim3(256), 0, st, c, r, few, qq, ldq, scale,
-                       window, oo, ldo, lse, fo, fm, err);
+                       window, oo, ldo, lse, reinterpret_cast<float*>(at(p.few.o_off)),
+                       reinterpret_cast<float2*>(at(p.few.ml_off)), reinterpret_cast<Join*>(at(p.few.join_off)),
+                       reinterpret_cast<int*>(at(p.few.count_off)), err);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if (p.many.joins) {
-    hipLaunchKernelGGL((paged_join_kernel<T, DH>), dim3(static_cast<unsigned>(p.many.joins), 8), dim3(256),
-                       0, st, c, r, many, window, mo, mm, oo, ldo, lse);
+  for (const PagedClass* k : {&p.many, &p.few}) {
+    if (!k->slots) continue;
+    hipLaunchKernelGGL((paged_join_kernel<T, DH>), dim3(static_cast<unsigned>(k->slots), k->tile / 16),
+                       dim3(256), 0, st, c, k->tile, reinterpret_cast<const Join*>(at(k->join_off)),
+                       reinterpret_cast<const int*>(at(k->count_off)), reinterpret_cast<const float*>(at(k->o_off)),
+                       reinterpret_cast<const float2*>(at(k->ml_off)), oo, ldo, lse);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  if (p.few.joins) {
-    hipLaunchKernelGGL((paged_join_kernel<T, DH>), dim3(static_cast<unsigned>(p.few.joins), p.few.tile / 8), dim3(256), 0,
-                       st, c, r, few, window, fo, fm, oo, ldo, lse);
-    e = hipGetLastError();
   }
   return e;
 }

@@ -282,28 +282,29 @@ sps_status check_paged_rows(const sps_paged_config& c, bool ragged, int rows, in
 }
 
 namespace {
-// The class of sequences that have up to `most` query rows each; `at` is the
-// workspace's end so far.
-PagedClass paged_class(const sps_paged_config& c, int tile, int target, long rows, size_t* at) {
+// A class with up to `tiles` tiles of query rows; `at` is the workspace's end so far.
+PagedClass paged_class(const sps_paged_config& c, int tile, int target, long tiles, size_t* at) {
   PagedClass k{};
-  const int G = c.n_heads / c.n_kv_heads;
   k.tile = tile;
   k.target = target;
-  // Every sequence's last tile may be partly filled.
-  const long tiles = (rows * G / tile + std::min<long>(c.B, rows)) * c.n_kv_heads;
+  tiles *= c.n_kv_heads;
   const long blocks = (static_cast<long>(c.max_pages) * c.page_size) / 32;
   const long ranges = (blocks + kPagedMinBlocks - 1) / kPagedMinBlocks;
-  // A sequence of n blocks has at most n / per + 1 ranges, and per is at least
-  // (all tiles' blocks) / target, so the ranges are at most target plus one a
-  // tile; only tiles of two ranges or more leave partials, at most twice
-  // their n / per.
-  k.items = std::min(tiles * ranges, tiles + target);
-  k.slots = ranges > 1 ? std::min(k.items, 2L * target) : 0;
-  k.joins = std::min(tiles, k.slots / 2);
+  // Up to 64 sequences, splitting stops at kPagedMostItems x target items
+  // (unsplit there is one a tile). With more, a sequence of n blocks has at
+  // most n / per + 1 ranges and per is at least (all tiles' blocks) / target:
+  // at most target ranges plus one a tile, and the tiles of two ranges or more
+  // have at most twice their n / per.
+  k.items = std::min(tiles * ranges, std::max(tiles + target, static_cast<long>(kPagedMostItems) * target));
+  k.slots = ranges > 1 ? std::min(k.items, static_cast<long>(kPagedMostItems) * target) : 0;
   k.o_off = *at;
   *at = align256(*at + static_cast<size_t>(k.slots) * tile * c.head_dim * 4);
   k.ml_off = *at;
   *at = align256(*at + static_cast<size_t>(k.slots) * tile * 8);
+  k.join_off = *at;
+  *at = align256(*at + static_cast<size_t>(k.slots) * kPagedJoinBytes);
+  k.count_off = *at;
+  *at += 256;
   return k;
 }
 }  // namespace
@@ -312,13 +313,17 @@ PagedPlan paged_plan(const sps_paged_config& c, bool ragged, int rows, int max_t
   PagedPlan p{};
   const int G = c.n_heads / c.n_kv_heads;
   const long q = static_cast<long>(std::min(rows, max_tokens)) * G;
-  // Up to 64 query rows: one tile of the smallest size that holds them.
-  // Among prompts of a ragged batch, those of up to 8 tokens.
-  const long few = q <= 64 ? q : ragged ? 8L * G : 0;
-  p.qt = static_cast<int>(std::min<long>(4, (few + 15) / 16));
+  // Up to 48 query rows (fp32 32): one tile of the smallest size that holds
+  // them. Among prompts of a ragged batch, those of up to 8 tokens.
+  const long most = 16L * paged_few_tiles(c.dtype);
+  const long few = q <= most ? q : ragged && G <= most ? std::min(most, 8L * G) : 0;
+  p.qt = static_cast<int>((few + 15) / 16);
   p.limit = 16 * p.qt;
-  if (p.qt) p.few = paged_class(c, 16 * p.qt, 4 * kCUs, rows, &p.total);
-  if (q > p.limit) p.many = paged_class(c, 16 * kManyQt * kManyWaves, 2 * kCUs, rows, &p.total);
+  // One tile a sequence; every sequence's last tile may be partly filled.
+  const long seqs = std::min(c.B, rows);
+  if (p.qt) p.few = paged_class(c, p.limit, 2 * kCUs, seqs, &p.total);
+  constexpr int kTile = 16 * kManyQt * kManyWaves;
+  if (q > p.limit) p.many = paged_class(c, kTile, 2 * kCUs, static_cast<long>(rows) * G / kTile + seqs, &p.total);
   if (p.total == 0) p.total = 256;
   return p;
 }
@@ -330,7 +335,7 @@ size_t paged_workspace_bytes(const sps_paged_config* c, int rows, int max_tokens
   // Calls with fewer tokens per sequence have other tiles and may have more of them.
   size_t most = 256;
   const int G = c->n_heads / c->n_kv_heads;
-  for (long q : {16L, 32L, 48L, 64L, static_cast<long>(kMaxPagedRows) * 1024})
+  for (long q : {16L, 32L, 48L, static_cast<long>(kMaxPagedRows) * 1024})
     for (bool ragged : {false, true})
       most = std::max(most, paged_plan(*c, ragged, rows, static_cast<int>(std::max(1L, std::min<long>(max_tokens, q / G)))).total);
   return most;

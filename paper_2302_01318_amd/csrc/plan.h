@@ -192,19 +192,24 @@ sps_status check_paged_rows(const sps_paged_config& c, bool ragged, int rows, in
 // Attention over the pages. A work item is a tile of up to `tile` query rows
 // (a sequence's tokens x the query heads of one KV head) against a range of
 // 32-position blocks. Ranges are the same number of blocks for all sequences
-// of a class, chosen on the device from the actual lengths so that there are
-// about `target` items, no fewer than kPagedMinBlocks each. Items whose rows
+// of a class, chosen on the device from the actual lengths for the `target`
+// work-groups that the card holds at once. Items whose rows
 // have only one range write the output; the others leave partials in at most
 // `slots` slots of the workspace, which a second launch joins. Sequences with
 // up to `limit` query rows are one class (their waves take different
 // positions, qt 16-row tiles each), those with more the other (their waves
 // take different rows).
-constexpr int kPagedMinBlocks = 8;     // 256 positions
+constexpr int kPagedMinBlocks = 4;     // the fewest a range has: one per wave
+constexpr size_t kPagedJoinBytes = 20;   // sizeof(Join), paged_attention.hip
+constexpr int kPagedMostItems = 6;     // most items of a split call, in `target`s
+// Tiles of the first class that two waves per SIMD have registers for.
+constexpr int paged_few_tiles(int dtype) { return dtype == SPS_DTYPE_F32 ? 2 : 3; }
 constexpr int kManyWaves = 4, kManyQt = 2;
 struct PagedClass {
   int tile, target;
-  long items, slots, joins;            // the most there can be; items 0: no such sequence
-  size_t o_off, ml_off;                // workspace: partial outputs, (reference, sum) pairs
+  long items, slots;                   // the most there can be; items 0: no such sequence
+  size_t o_off, ml_off;                // workspace: partial outputs, (reference, sum) pairs,
+  size_t join_off, count_off;          // per slot what is to be joined, the number of slots in use
 };
 struct PagedPlan {
   int qt, limit;
