@@ -85,10 +85,11 @@ hipError_t launch_kv_copy(int dtype, int to_cache, void* kc, void* vc, int H, in
 // (linear) or by parts.
 struct RopeArgs {
   int rot, interleaved, by_parts;
+  int whole;               // heads split into runs of 8 elements that rotate alike (or not at all)
   float amp;
   double step, inv_factor, original, low, inv_span;
 };
-RopeArgs rope_args(const sps_rope_spec& r);
+RopeArgs rope_args(const sps_rope_spec* r, int DH);   // NULL: no rotation
 hipError_t launch_rope(int dtype, const void* x, int64_t ldx, const int32_t* positions, const RopeArgs& r, int rows,
                        int heads, int DH, bool backward, void* out, int64_t ldo, hipStream_t st);
 
@@ -105,7 +106,7 @@ struct PagedRows {
   int rows, max_tokens, pos_offset;
 };
 hipError_t launch_paged_append(int dtype, const PagedView& c, const PagedRows& r, const void* k, int64_t ldk,
-                               const void* v, int64_t ldv, const RopeArgs* rope, const void* q, int64_t ldq, void* qo,
+                               const void* v, int64_t ldv, const RopeArgs& rope, const void* q, int64_t ldq, void* qo,
                                int64_t ldqo, int* err, hipStream_t st);
 hipError_t launch_paged_attention(int dtype, const PagedView& c, const PagedRows& r, const PagedPlan& p, const void* q,
                                   int64_t ldq, float scale, int window, void* out, int64_t ldo, float* lse,

@@ -643,7 +643,7 @@ sps_status sps_rope(const void* x, int64_t x_stride, const int32_t* positions, c
   if (rows == 0) return SPS_OK;
   if (!x || !out || !positions || (x == out && x_stride != out_stride)) return SPS_E_INVALID;
   if (misaligned(x, dtype) || misaligned(out, dtype)) return SPS_E_INVALID;
-  SPS_HIP(sps::launch_rope(dtype, x, x_stride, positions, sps::rope_args(*spec), rows, heads, head_dim, backward != 0,
+  SPS_HIP(sps::launch_rope(dtype, x, x_stride, positions, sps::rope_args(spec, head_dim), rows, heads, head_dim, backward != 0,
                            out, out_stride, as_stream(stream)));
   return SPS_OK;
 }
@@ -689,10 +689,8 @@ sps_status sps_paged_append(sps_paged_t kv, int32_t layer, const void* k, int64_
     return SPS_E_INVALID;
   int* err = device_error_ptr();
   if (!err) return SPS_E_HIP;
-  sps::RopeArgs ra{};
-  if (rope) ra = sps::rope_args(*rope);
   SPS_HIP(sps::launch_paged_append(c.dtype, paged_view(kv, layer), {starts, rows, max_tokens, pos_offset}, k, k_stride,
-                                   v, v_stride, rope ? &ra : nullptr, q, q_stride, q_out, q_out_stride, err,
+                                   v, v_stride, sps::rope_args(rope, c.head_dim), q, q_stride, q_out, q_out_stride, err,
                                    as_stream(stream)));
   return SPS_OK;
 }
