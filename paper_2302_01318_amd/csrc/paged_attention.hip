@@ -37,9 +37,10 @@ struct Place {
 };
 
 // Sequences with more than `above` and up to `limit` query rows, in tiles of
-// `tile` (plan.h). split: the cost of an item's partials in blocks.
+// `tile` (plan.h). What an item costs beside its blocks, in blocks: own, and
+// where it is one of several ranges split more for its partials.
 struct Class {
-  int tile, target, above, limit, split;
+  int tile, target, above, limit, own, split;
 };
 
 // What the second launch has to join: entry i of the slots' descriptors, if i
@@ -58,14 +59,29 @@ __device__ __forceinline__ int2 tiles_blocks(const PagedView& c, const Class& k,
                    (end + 31) / 32 - lo / 32);
 }
 
+// The smallest of 64 lanes' values, with DPP moves (lanes without a source keep theirs).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_min(float v) {
+  const int x = __builtin_bit_cast(int, v);
+  return fminf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(x, x, CTRL, ROWS, 0xf, false)));
+}
+__device__ __forceinline__ float wave_min_dpp(float v) {
+  v = dpp_min<0x111, 0xf>(v);   // row_shr:1 .. 8, then across the rows of 16: lane 63 has it
+  v = dpp_min<0x112, 0xf>(v);
+  v = dpp_min<0x114, 0xf>(v);
+  v = dpp_min<0x118, 0xf>(v);
+  v = dpp_min<0x142, 0xa>(v);
+  v = dpp_min<0x143, 0xc>(v);
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+
 // Blocks per range, by up to 64 sequences' tiles and blocks (one a lane): lane
 // r - 1 prices r ranges of the longest, in the time of a block: the rounds that
 // the items take over the card's `target` slots, or where sizes or rounds are
 // uneven the work per slot and most of an item until the last one ends
-// (work-groups go faster as others end). An item costs kItemBlocks beside its
-// blocks, one of several ranges k.split more for its partials, and the joining
-// kJoinBlocks. Every lane takes the cheapest.
-constexpr int kItemBlocks = 4, kJoinBlocks = 3;
+// (work-groups go faster as others end). Joining costs kJoinBlocks. Every lane
+// takes the cheapest.
+constexpr int kJoinBlocks = 3;
 __device__ __forceinline__ int blocks_per_range(const PagedView& c, const Class& k, int tiles, int blocks) {
   const int lane = threadIdx.x & 63;
   int most = 0;
@@ -82,16 +98,13 @@ __device__ __forceinline__ int blocks_per_range(const PagedView& c, const Class&
     work += static_cast<float>(t) * (n - per + 1);
   }
   const bool split = lane && per < most;
-  const float own = static_cast<float>(kItemBlocks + (split ? k.split : 0));
+  const float own = static_cast<float>(k.own + (split ? k.split : 0));
   const float n = static_cast<float>(items) * c.H, slots = static_cast<float>(k.target);
   const float each = min(per, most) + own;
   float cost = fminf(ceilf(n / slots) * each, (work * c.H + n * own) / fminf(n, slots) + 0.75f * each);
   if (split) cost += kJoinBlocks;
   if (lane && n > kPagedMostItems * slots) cost = INFINITY;        // the workspace's bound
-  float best = cost;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) best = fminf(best, __shfl_xor(best, o));
-  const uint64_t cheapest = __ballot(cost == best);
+  const uint64_t cheapest = __ballot(cost == wave_min_dpp(cost));
   return cheapest ? __builtin_amdgcn_readlane(per, __ffsll(static_cast<unsigned long long>(cheapest)) - 1) : kPagedMinBlocks;
 }
 
@@ -129,7 +142,7 @@ __device__ __forceinline__ bool find_place(const PagedView& c, const PagedRows& 
   const int kvh = idx - want * c.H;
   uint64_t before = 0;
   bool found = false;
-  if (c.B <= 64) {
+  if (c.B <= kMaxFew) {
     // A sequence a lane, in registers.
     SeqRows s{};
     if (lane < c.B) s = seq_rows(c, r, lane);
@@ -181,7 +194,7 @@ __device__ __forceinline__ void leave_join(const PagedView& c, const Place& pl, 
         Join{pl.s.r0, pl.s.n * c.G, pl.tile, pl.kvh, pl.range == 0 ? pl.ranges : 0};
 }
 
-template <typename T> __device__ __forceinline__ bool nonfinite(T x);
+template <typename T> __device__ __forceinline__ bool nonfinite(T x);  // Inf or NaN
 template <> __device__ __forceinline__ bool nonfinite<bf16>(bf16 x) {
   return (__builtin_bit_cast(unsigned short, x) & 0x7f80) == 0x7f80;
 }
@@ -269,22 +282,22 @@ __device__ __forceinline__ void softmax_weights(f32x4 (&s)[NP], RowSoftmax& w) {
     }
 }
 
+// The values of positions past the last one, which may hold anything, cleared.
+template <typename T>
+__device__ __forceinline__ void clear_past(Frag<T>& vf, int pos0, int end, int grp) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (pos0 + (e >> 2) * 16 + grp * 4 + (e & 3) >= end) vf.v[e] = from_f32<T>(0.f);
+}
+
 // Values of a block in which some row of the tile does not see some position:
 // 0 x Inf would carry a value that is not finite into the rows that do not see
-// it. Positions past the last one (they may hold anything) are cleared; other
-// values that are not finite are taken out of the fragment too, and put into
-// the rows that see them by counting, per row and dim, visible +Inf, -Inf and
-// NaN with products of ones.
+// it. Such values are taken out of the fragment, and put into the rows that see
+// them by counting, per row and dim, visible +Inf, -Inf and NaN with products
+// of ones.
 template <typename T, int QT, int ND>
 __device__ __forceinline__ void clean_values(Frag<T>& vf, int pos0, const int (&qpos)[QT], int window, int end, int grp,
                                              f32x4 (&o)[QT][ND], int dt) {
-  bool odd = false;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    if (pos0 + (e >> 2) * 16 + grp * 4 + (e & 3) >= end) vf.v[e] = from_f32<T>(0.f);
-    odd |= nonfinite(vf.v[e]);
-  }
-  if (!__ballot(odd)) return;
 #pragma unroll 1
   for (int kind = 0; kind < 3; ++kind) {
     const float what = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
@@ -313,49 +326,56 @@ __device__ __forceinline__ void clean_values(Frag<T>& vf, int pos0, const int (&
     if (nonfinite(vf.v[e])) vf.v[e] = from_f32<T>(0.f);
 }
 
-// Row `in` of a tile (its dims 16 dt + 4 grp .. + 3 in this lane): the output,
-// or a partial if the tile has more ranges.
-template <typename T, int DH>
+// Row `in` of a tile, of its dims 16 dt .. 16 (dt + N) - 1 the runs 4 grp .. + 3 of
+// 16: the output, or a partial if the tile has more ranges.
+template <typename T, int DH, int N>
 __device__ __forceinline__ void write_row(const PagedView& c, const Class& k, const Place& pl, int in, int tok, int head,
-                                          int grp, float ref, float l, const f32x4 (&o)[DH / 16], T* out, int64_t ldo,
+                                          int grp, int dt, float ref, float l, const f32x4 (&o)[N], T* out, int64_t ldo,
                                           float* lse, float* part_o, float2* part_ml) {
+  const bool first = grp == 0 && dt == 0;
   if (pl.ranges > 1) {
     const size_t at = (pl.slot + static_cast<long>(pl.range) * c.H) * k.tile + in;
-    if (grp == 0) part_ml[at] = make_float2(ref, l);
+    if (first) part_ml[at] = make_float2(ref, l);
 #pragma unroll
-    for (int dt = 0; dt < DH / 16; ++dt) *reinterpret_cast<f32x4*>(part_o + at * DH + dt * 16 + grp * 4) = o[dt];
+    for (int d = 0; d < N; ++d) *reinterpret_cast<f32x4*>(part_o + at * DH + (dt + d) * 16 + grp * 4) = o[d];
     return;
   }
   // A sum of zero: no visible position, or none with weight.
   const float inv = 1.f / l;
-  T* dst = out + tok * ldo + head * DH + grp * 4;
+  T* dst = out + tok * ldo + head * DH + dt * 16 + grp * 4;
 #pragma unroll
-  for (int dt = 0; dt < DH / 16; ++dt) store4_any(dst + dt * 16, l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[dt] * inv);
-  if (lse && grp == 0)
+  for (int d = 0; d < N; ++d) store4_any(dst + d * 16, l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o[d] * inv);
+  if (lse && first)
     lse[static_cast<size_t>(tok) * c.H * c.G + head] = l == 0.f ? -INFINITY : 0.69314718f * ref + logf(l);
 }
 
+// LDS of a work-group whose sequences have up to QT tiles.
 template <typename T, int DH, int QT>
-__global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedView c, PagedRows r, Class k,
-                                                         const T* __restrict__ q, int64_t ldq, float scale, int window,
-                                                         T* __restrict__ out, int64_t ldo, float* __restrict__ lse,
-                                                         float* __restrict__ part_o, float2* __restrict__ part_ml,
-                                                         Join* __restrict__ joins, int* __restrict__ count, int* err) {
-  constexpr int TR = 16 * QT, ND = DH / 16;
-  // The plan's words per sequence, then two waves' (O, max, sum).
-  constexpr int kMergeF4 = 2 * QT * ND * 64, kPlanF4 = 2 * kMaxPagedB / 4;
-  __shared__ f32x4 sm[kMergeF4 > kPlanF4 ? kMergeF4 : kPlanF4];
-  __shared__ float2 sml[2 * QT * 64];
-  Place pl;
-  if (!find_place(c, r, window, k, reinterpret_cast<int*>(sm), count, err, &pl)) return;
-  leave_join(c, pl, joins);
+struct FewLds {
+  // The plan's words per sequence, then two waves' (O, reference, sum), or with one tile all four's.
+  static constexpr int kF4 = (QT > 2 ? 2 * QT : 4) * (DH / 16) * 64, kPlanF4 = 2 * kMaxPagedB / 4;
+  f32x4 o[kF4 > kPlanF4 ? kF4 : kPlanF4];
+  float2 ml[(QT > 2 ? 2 * QT : 4) * 64];
+  Frag<T> q[QT > 1 || sizeof(T) == 4 ? QT * (DH / 32) * 64 : 1];
+};
+
+// An item of QT tiles.
+template <typename T, int DH, int QT, typename Lds>
+__device__ __forceinline__ void few_item(const PagedView& c, const Class& k, const Place& pl, const T* __restrict__ q,
+                                         int64_t ldq, float scale, int window, T* __restrict__ out, int64_t ldo,
+                                         float* __restrict__ lse, float* __restrict__ part_o,
+                                         float2* __restrict__ part_ml, int* err, Lds& lds) {
+  constexpr int ND = DH / 16;
+  f32x4* sm = lds.o;
+  float2* sml = lds.ml;
+  Frag<T>* sq = lds.q;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int r16 = lane & 15, grp = lane >> 4;
   const SeqRows& s = pl.s;
   const int cap = c.max_pages << c.page_log2;
-  const int nrows = s.n * c.G, row0 = pl.tile * TR;
+  const int nrows = s.n * c.G, row0 = 0;
   // Positions of the tile's first and last token, and what they see.
-  const int first = s.p0 + uniform(row0 / c.G), last = s.p0 + uniform((min(row0 + TR, nrows) - 1) / c.G);
+  const int first = s.p0 + uniform(row0 / c.G), last = s.p0 + uniform((nrows - 1) / c.G);
   const int end = min(max(last + 1, 0), cap);
   const int lo = window ? min(max(first - window + 1, 0), end) : 0;
   const int base = (window ? min(max(s.p0 - window + 1, 0), min(max(s.p0 + s.n, 0), cap)) : 0) / 32;
@@ -365,7 +385,6 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedView c, PagedRow
   // The queries' fragments, in registers or (kStaged: more than a 16-row tile,
   // or fp32) in LDS, where all waves read them: two waves per SIMD need the room.
   constexpr bool kStaged = QT > 1 || sizeof(T) == 4;
-  __shared__ Frag<T> sq[kStaged ? QT * (DH / 32) * 64 : 1];
   Frag<T> qf[kStaged ? 1 : DH / 32];
   int qpos[QT], tok[QT], head[QT];
 #pragma unroll
@@ -509,8 +528,18 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedView c, PagedRow
     }
     softmax_scale(sc, c_log2, w, o);
     if (masked) {
+      if (pos0 + 32 > end) {
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt) clean_values(vf[dt], pos0, qpos, window, end, grp, o, dt);
+        for (int dt = 0; dt < ND; ++dt) clear_past(vf[dt], pos0, end, grp);
+      }
+      // The values times zero: NaN if one of them is not finite.
+      f32x4 zero{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) zero = mma8(zero, vf[dt], Frag<T>::zero());
+      if (__ballot(zero[0] + zero[1] + zero[2] + zero[3] != 0.f)) {
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) clean_values(vf[dt], pos0, qpos, window, end, grp, o, dt);
+      }
     }
     products(sc);
     i = seek(i + 1);
@@ -520,7 +549,6 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedView c, PagedRow
     }
   }
 
-  // Waves 2, 3 into 0, 1, then 1 into 0.
   float ref[QT], sum[QT];
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {
@@ -528,6 +556,34 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedView c, PagedRow
     sum[qt] = w[qt].sum + __shfl_xor(w[qt].sum, 16);
     sum[qt] += __shfl_xor(sum[qt], 32);
   }
+  if constexpr (QT == 1) {
+    // Every wave joins a quarter of the dims.
+    sml[wave * 64 + lane] = make_float2(ref[0], sum[0]);
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) sm[(wave * ND + dt) * 64 + lane] = o[0][dt];
+    __syncthreads();
+    float2 ml[4];
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      ml[x] = sml[x * 64 + lane];
+      m = fmaxf(m, ml[x].x);
+    }
+    const float mu = m == -INFINITY ? 0.f : m;
+    f32x4 part[ND / 4] = {};
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float a = fast_exp2(ml[x].x - mu);
+      l += a * ml[x].y;
+#pragma unroll
+      for (int d = 0; d < ND / 4; ++d) part[d] += a * sm[(x * ND + wave * (ND / 4) + d) * 64 + lane];
+    }
+    if (row0 + r16 < nrows)
+      write_row<T, DH, ND / 4>(c, k, pl, r16, tok[0], head[0], grp, wave * (ND / 4), m, l, part, out, ldo, lse, part_o,
+                               part_ml);
+    return;
+  }
+  // Waves 2, 3 into 0, 1, then 1 into 0.
 #pragma unroll
   for (int half = 2; half; half >>= 1) {
     if (wave >= half && wave < 2 * half) {
@@ -557,8 +613,29 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedView c, PagedRow
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt)
     if (row0 + qt * 16 + r16 < nrows)
-      write_row<T, DH>(c, k, pl, qt * 16 + r16, tok[qt], head[qt], grp, ref[qt], sum[qt], o[qt], out, ldo, lse, part_o,
-                       part_ml);
+      write_row<T, DH, ND>(c, k, pl, qt * 16 + r16, tok[qt], head[qt], grp, 0, ref[qt], sum[qt], o[qt], out, ldo, lse,
+                           part_o, part_ml);
+}
+
+// The tiles an item has are its sequence's (k.tile holds all its rows): its own
+// straight code for each number of them, up to QT.
+template <typename T, int DH, int QT>
+__global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedView c, PagedRows r, Class k, const T* __restrict__ q,
+                                                           int64_t ldq, float scale, int window, T* __restrict__ out,
+                                                           int64_t ldo, float* __restrict__ lse,
+                                                           float* __restrict__ part_o, float2* __restrict__ part_ml,
+                                                           Join* __restrict__ joins, int* __restrict__ count, int* err) {
+  __shared__ FewLds<T, DH, QT> lds;
+  Place pl;
+  if (!find_place(c, r, window, k, reinterpret_cast<int*>(lds.o), count, err, &pl)) return;
+  leave_join(c, pl, joins);
+  const int tiles = (pl.s.n * c.G + 15) / 16;
+  if (tiles <= 1)
+    few_item<T, DH, 1>(c, k, pl, q, ldq, scale, window, out, ldo, lse, part_o, part_ml, err, lds);
+  else if (QT > 1 && (QT == 2 || tiles == 2))
+    few_item<T, DH, QT < 2 ? QT : 2>(c, k, pl, q, ldq, scale, window, out, ldo, lse, part_o, part_ml, err, lds);
+  else if (QT > 2)
+    few_item<T, DH, QT>(c, k, pl, q, ldq, scale, window, out, ldo, lse, part_o, part_ml, err, lds);
 }
 
 // The ranges of a tile's rows joined: 16 lanes per row, four rows per wave (one
@@ -742,7 +819,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
     return f;
   };
   uint32_t there = blk0 < blk1 ? fetch(blk0, 0) : 0, next = 0, on = 0;
-  bool ready = false;
+  bool ready = false, fresh = true;                // fresh: no reference yet
   int b = 0, blk = blk0;
   while (blk < blk1) {
     // Stages that every row of the wave sees all of, and whose scores need no
@@ -760,7 +837,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
           on |= pos0 + h * 32 <= wlast && !(window && pos0 + h * 32 + 31 <= wfirst - window) ? there & 1u << h : 0;
         ready = true;
       }
-      if (on != (1u << NB) - 1 || pos0 + NB * 32 - 1 > min(wfirst, end - 1) || (window && pos0 <= wlast - window)) break;
+      if (fresh || on != (1u << NB) - 1 || pos0 + NB * 32 - 1 > min(wfirst, end - 1) || (window && pos0 <= wlast - window)) break;
       f32x4 sc[QT][2 * NB];
       scores(sc, b, 0);
       bool up = false;
@@ -797,16 +874,20 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
     }
     if (blk >= blk1) break;
     // The others block by block.
+    fresh = false;
 #pragma unroll 1
     for (int h = 0; h < NB; ++h) {
       if (!(on >> h & 1)) continue;
       const int pos0 = (blk + h) * 32;
+      const bool masked = pos0 + 31 > min(wfirst, end - 1) || (window && pos0 <= wlast - window);
       f32x4 sc[QT][2];
       scores(sc, b, h);
+      if (masked) {
 #pragma unroll
-      for (int qt = 0; qt < QT; ++qt)
+        for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
-        for (int pt = 0; pt < 2; ++pt) mask_scores(pos0 + pt * 16, qpos[qt], window, end, grp, sc[qt][pt]);
+          for (int pt = 0; pt < 2; ++pt) mask_scores(pos0 + pt * 16, qpos[qt], window, end, grp, sc[qt][pt]);
+      }
       softmax_scale(sc, c_log2, w, o);
       Frag<T> pf[QT];
 #pragma unroll
@@ -814,23 +895,31 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
         softmax_weights(sc[qt], w[qt]);
         pf[qt] = rounded(sc[qt][0], sc[qt][1]);
       }
-      // The values times zero: NaN if one of them is not finite.
-      f32x4 zero{0.f, 0.f, 0.f, 0.f};
+      bool plain = !masked;
+      if (masked && pos0 + 32 <= end) {
+        // The values times zero: NaN if one of them is not finite.
+        f32x4 zero{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt)
-        zero = mma8(zero, load_frag(&stage[b][h][1][(dt * 64 + lane) * 8]), Frag<T>::zero());
-      if (__ballot(zero[0] + zero[1] + zero[2] + zero[3] != 0.f) || pos0 + 32 > end) {
+        for (int dt = 0; dt < ND; ++dt)
+          zero = mma8(zero, load_frag(&stage[b][h][1][(dt * 64 + lane) * 8]), Frag<T>::zero());
+        plain = !__ballot(zero[0] + zero[1] + zero[2] + zero[3] != 0.f);
+      }
+      if (plain) {
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) {
-          Frag<T> vf = load_frag(&stage[b][h][1][(dt * 64 + lane) * 8]);
-          clean_values(vf, pos0, qpos, window, end, grp, o, dt);
+          const Frag<T> vf = load_frag(&stage[b][h][1][(dt * 64 + lane) * 8]);
 #pragma unroll
           for (int qt = 0; qt < QT; ++qt) o[qt][dt] = mma8(o[qt][dt], vf, pf[qt]);
         }
       } else {
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) {
-          const Frag<T> vf = load_frag(&stage[b][h][1][(dt * 64 + lane) * 8]);
+          Frag<T> vf = load_frag(&stage[b][h][1][(dt * 64 + lane) * 8]);
+          clear_past(vf, pos0, end, grp);
+          bool odd = false;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) odd |= nonfinite(vf.v[e]);
+          if (__ballot(odd)) clean_values(vf, pos0, qpos, window, end, grp, o, dt);
 #pragma unroll
           for (int qt = 0; qt < QT; ++qt) o[qt][dt] = mma8(o[qt][dt], vf, pf[qt]);
         }
@@ -848,8 +937,8 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
     const int row = wrow0 + qt * 16 + r16;
     if (row < nrows) {
       const int t = row / c.G;
-      write_row<T, DH>(c, k, pl, row - row0, s.r0 + t, pl.kvh * c.G + row - t * c.G, grp, w[qt].ref(), sum, o[qt], out,
-                       ldo, lse, part_o, part_ml);
+      write_row<T, DH, ND>(c, k, pl, row - row0, s.r0 + t, pl.kvh * c.G + row - t * c.G, grp, 0, w[qt].ref(), sum, o[qt],
+                           out, ldo, lse, part_o, part_ml);
     }
   }
 }
@@ -869,12 +958,14 @@ static hipError_t attn_t(const PagedView& c, const PagedRows& r, const PagedPlan
                          hipStream_t st) {
   const T* qq = static_cast<const T*>(q);
   T* oo = static_cast<T*>(out);
-  const Class few{p.few.tile, p.few.target, 0, p.limit, p.qt}, many{p.many.tile, p.many.target, p.limit, INT32_MAX, 16};
+  // Blocks take about 1 us; an item's start 4 (8: its queries and first stage), a partial of 128 rows 20.
+  const Class few{p.few.tile, p.few.target, 0, p.limit, 4, p.qt}, many{p.many.tile, p.many.target, p.limit, INT32_MAX, 8, 20};
   auto at = [&](size_t off) { return ws + off; };
   hipError_t e = hipSuccess;
   if (p.many.items) {
-    hipLaunchKernelGGL((paged_many_kernel<T, DH, kManyQt, kManyWaves>), dim3(static_cast<unsigned>(p.many.items)),
-                       dim3(64 * kManyWaves), 0, st, c, r, many, qq, ldq, scale, window, oo, ldo, lse,
+    constexpr int kQt = sizeof(T) == 2 ? 2 : 1, kWaves = kManyTile / (16 * kQt);
+    hipLaunchKernelGGL((paged_many_kernel<T, DH, kQt, kWaves>), dim3(static_cast<unsigned>(p.many.items)),
+                       dim3(64 * kWaves), 0, st, c, r, many, qq, ldq, scale, window, oo, ldo, lse,
                        reinterpret_cast<float*>(at(p.many.o_off)), reinterpret_cast<float2*>(at(p.many.ml_off)),
                        reinterpret_cast<Join*>(at(p.many.join_off)), reinterpret_cast<int*>(at(p.many.count_off)), err);
     if ((e = hipGetLastError()) != hipSuccess) return e;

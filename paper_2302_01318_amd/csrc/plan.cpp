@@ -290,13 +290,14 @@ PagedClass paged_class(const sps_paged_config& c, int tile, int target, long til
   tiles *= c.n_kv_heads;
   const long blocks = (static_cast<long>(c.max_pages) * c.page_size) / 32;
   const long ranges = (blocks + kPagedMinBlocks - 1) / kPagedMinBlocks;
-  // Up to 64 sequences, splitting stops at kPagedMostItems x target items
+  // Up to kMaxFew sequences, splitting stops at kPagedMostItems x target items
   // (unsplit there is one a tile). With more, a sequence of n blocks has at
   // most n / per + 1 ranges and per is at least (all tiles' blocks) / target:
   // at most target ranges plus one a tile, and the tiles of two ranges or more
   // have at most twice their n / per.
-  k.items = std::min(tiles * ranges, std::max(tiles + target, static_cast<long>(kPagedMostItems) * target));
-  k.slots = ranges > 1 ? std::min(k.items, static_cast<long>(kPagedMostItems) * target) : 0;
+  const long most = static_cast<long>(kPagedMostItems) * target;
+  k.items = std::min(tiles * ranges, c.B <= kMaxFew ? std::max(tiles, most) : tiles + target);
+  k.slots = ranges > 1 ? std::min(k.items, most) : 0;
   k.o_off = *at;
   *at = align256(*at + static_cast<size_t>(k.slots) * tile * c.head_dim * 4);
   k.ml_off = *at;
@@ -322,8 +323,7 @@ PagedPlan paged_plan(const sps_paged_config& c, bool ragged, int rows, int max_t
   // One tile a sequence; every sequence's last tile may be partly filled.
   const long seqs = std::min(c.B, rows);
   if (p.qt) p.few = paged_class(c, p.limit, 2 * kCUs, seqs, &p.total);
-  constexpr int kTile = 16 * kManyQt * kManyWaves;
-  if (q > p.limit) p.many = paged_class(c, kTile, 2 * kCUs, static_cast<long>(rows) * G / kTile + seqs, &p.total);
+  if (q > p.limit) p.many = paged_class(c, kManyTile, 2 * kCUs, static_cast<long>(rows) * G / kManyTile + seqs, &p.total);
   if (p.total == 0) p.total = 256;
   return p;
 }

@@ -201,10 +201,13 @@ sps_status check_paged_rows(const sps_paged_config& c, bool ragged, int rows, in
 // take different rows).
 constexpr int kPagedMinBlocks = 4;     // the fewest a range has: one per wave
 constexpr size_t kPagedJoinBytes = 20;   // sizeof(Join), paged_attention.hip
-constexpr int kPagedMostItems = 6;     // most items of a split call, in `target`s
+constexpr int kPagedMostItems = 2;     // most items of a split call, in `target`s (what is left of a grid still has to start)
 // Tiles of the first class that two waves per SIMD have registers for.
 constexpr int paged_few_tiles(int dtype) { return dtype == SPS_DTYPE_F32 ? 2 : 3; }
-constexpr int kManyWaves = 4, kManyQt = 2;
+// The second class: a tile of 128 rows, in four waves of two 16-row tiles, or
+// in fp32, for the registers, eight of one.
+constexpr int kManyTile = 128;
+constexpr int kMaxFew = 64;            // sequences whose ranges are priced (paged_attention.hip)
 struct PagedClass {
   int tile, target;
   long items, slots;                   // the most there can be; items 0: no such sequence

@@ -397,39 +397,43 @@ def fp8_decode(codes):
     return out
 
 
-def _raw_stream(dev):
-    return torch._C._cuda_getCurrentRawStream(dev)
+# The checks below run on every call of operators that take a few microseconds.
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
-def _here(t, dtype, name):
-    """The current device, on which the library runs its calls, if t is one of its tensors of `dtype`."""
+def _here():
+    """The current device, on which the library runs its calls (-2: none, no tensor's)."""
+    if torch.cuda.is_initialized():
+        return _current_device()
+    return torch.cuda.current_device() if torch.cuda.is_available() else -2
+
+
+def _refuse(t, dev, shape, dtype, name):
     if not t.is_cuda:
         raise ValueError("%s must be a device tensor" % name)
-    dev = torch.cuda.current_device()
     if t.get_device() != dev:
         raise ValueError("%s is on device %d, the current device is %d" % (name, t.get_device(), dev))
     if t.dtype != dtype:
         raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    return dev
+    raise ValueError("%s must be %s, got %s with strides %s" % (name, tuple(shape), tuple(t.shape), t.stride()))
 
 
-def _heads(t, rows, heads, dim, dtype, name):
+def _heads(t, dev, shape, dtype, name):
     """(address, row stride) of a [rows][heads][dim] tensor whose rows may lie
     apart (a slice of a wider one), each row's heads one after the other."""
-    _here(t, dtype, name)
-    if t.shape != (rows, heads, dim):
-        raise ValueError("%s must be [%d][%d][%d], got %s" % (name, rows, heads, dim, tuple(t.shape)))
-    s = t.stride()
-    if s[2] != 1 or (heads > 1 and s[1] != dim):
-        raise ValueError("%s: the heads of a row must lie one after the other" % name)
-    return t.data_ptr(), s[0] if rows > 1 else heads * dim
+    if t.get_device() != dev or t.dtype is not dtype or t.shape != shape:
+        _refuse(t, dev, shape, dtype, name)
+    rows, heads, dim = shape
+    r, h, d = t.stride()
+    if d != 1 or (h != dim and heads > 1):
+        _refuse(t, dev, shape, dtype, name)
+    return t.data_ptr(), r if rows > 1 else heads * dim
 
 
-def _flat(t, shape, dtype, name):
+def _flat(t, dev, shape, dtype, name):
     """Address of a contiguous tensor of that shape."""
-    _here(t, dtype, name)
-    if t.shape != shape or not t.is_contiguous():
-        raise ValueError("%s must be contiguous %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if t.get_device() != dev or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        _refuse(t, dev, shape, dtype, name)
     return t.data_ptr()
 
 
@@ -437,19 +441,25 @@ def rope(x, positions, spec, out=None, backward=False):
     """x [rows][heads][head_dim] (bf16 or fp32; rows may lie apart) rotated at
     the int32 positions [rows], or with backward=True the gradient of that.
     out may be x itself."""
-    if x.dim() != 3:
-        raise ValueError("x must be [rows][heads][head_dim], got %s" % (tuple(x.shape),))
-    if x.dtype != torch.float32 and x.dtype != torch.bfloat16:
-        raise ValueError("x must be float32 or bfloat16, got %s" % x.dtype)
-    rows, heads, dim = x.shape
-    dev = _here(x, x.dtype, "x")
+    shape, dt = x.shape, x.dtype
+    if len(shape) != 3:
+        raise ValueError("x must be [rows][heads][head_dim], got %s" % (tuple(shape),))
+    if dt is torch.bfloat16:
+        code = 1
+    elif dt is torch.float32:
+        code = 0
+    else:
+        raise ValueError("x must be float32 or bfloat16, got %s" % dt)
+    dev = _here()
+    xp, xs = _heads(x, dev, shape, dt, "x")
     if out is None:
-        out = torch.empty((rows, heads, dim), dtype=x.dtype, device=x.device)
-    xp, xs = _heads(x, rows, heads, dim, x.dtype, "x")
-    op, os_ = _heads(out, rows, heads, dim, x.dtype, "out")
-    check(lib.sps_rope(xp, xs, _flat(positions, (rows,), torch.int32, "positions"), ctypes.byref(spec), rows, heads,
-                       dim, 0 if x.dtype == torch.float32 else 1, 1 if backward else 0, op, os_, _raw_stream(dev)),
-          "sps_rope")
+        out = torch.empty(shape, dtype=dt, device=x.device)
+    op, os_ = _heads(out, dev, shape, dt, "out")
+    rows, heads, dim = shape
+    st = lib.sps_rope(xp, xs, _flat(positions, dev, (rows,), torch.int32, "positions"), ctypes.byref(spec), rows, heads,
+                      dim, code, backward, op, os_, _raw_stream(dev))
+    if st:
+        check(st, "sps_rope")
     return out
 
 
@@ -475,19 +485,20 @@ class PagedKV:
         if lengths is None:
             lengths = torch.zeros(B, dtype=torch.int32, device=device)
         self.buf, self.page_table, self.lengths = buf, page_table, lengths
+        self.dev = buf.get_device()
         self.handle = c_void_p()
         self._destroy = lib.sps_paged_destroy   # see Model.__init__
-        check(lib.sps_paged_create(ctypes.byref(self.cfg), _flat(buf, shape, self.dtype, "buf"),
-                                   _flat(page_table, (B, max_pages), torch.int32, "page_table"),
-                                   _flat(lengths, (B,), torch.int32, "lengths"), ctypes.byref(self.handle)),
+        dev = _here()
+        check(lib.sps_paged_create(ctypes.byref(self.cfg), _flat(buf, dev, shape, self.dtype, "buf"),
+                                   _flat(page_table, dev, (B, max_pages), torch.int32, "page_table"),
+                                   _flat(lengths, dev, (B,), torch.int32, "lengths"), ctypes.byref(self.handle)),
               "sps_paged_create")
 
-    def _rows(self, rows, starts, max_tokens):
-        if starts is None:
-            if max_tokens is None:
-                max_tokens = rows // self.B
-            return None, max_tokens
-        return _flat(starts, (self.B + 1,), torch.int32, "starts"), rows if max_tokens is None else max_tokens
+    def _device(self):
+        dev = _current_device()
+        if dev != self.dev:
+            raise ValueError("the cache is on device %d, the current device is %d" % (self.dev, dev))
+        return dev
 
     def append(self, layer, k, v, rope=None, q=None, q_out=None, starts=None, max_tokens=None, pos_offset=0):
         """Write the new tokens' k and v [rows][n_kv_heads][head_dim] into their
@@ -495,23 +506,29 @@ class PagedKV:
         [rows][n_heads][head_dim] return the queries rotated alike (in q_out,
         which may be q). Sequence b has rows starts[b] .. starts[b + 1] - 1, or
         rows / B each; at most max_tokens (default: rows)."""
-        H, D, dt = self.n_kv_heads, self.head_dim, self.dtype
-        rows = k.shape[0]
-        dev = _here(self.buf, dt, "the cache")
-        kp, ks = _heads(k, rows, H, D, dt, "k")
-        vp, vs = _heads(v, rows, H, D, dt, "v")
-        qp = qop = None
-        qs = qos = 0
+        dt, rows, dev = self.dtype, k.shape[0], self._device()
+        shape = (rows, self.n_kv_heads, self.head_dim)
+        kp, ks = _heads(k, dev, shape, dt, "k")
+        vp, vs = _heads(v, dev, shape, dt, "v")
         if q is not None:
-            qp, qs = _heads(q, rows, self.n_heads, D, dt, "q")
+            shape = (rows, self.n_heads, self.head_dim)
+            qp, qs = _heads(q, dev, shape, dt, "q")
             if q_out is None:
-                q_out = torch.empty((rows, self.n_heads, D), dtype=dt, device=q.device)
-            qop, qos = _heads(q_out, rows, self.n_heads, D, dt, "q_out")
-        elif q_out is not None:
+                q_out = torch.empty(shape, dtype=dt, device=q.device)
+            qop, qos = _heads(q_out, dev, shape, dt, "q_out")
+        elif q_out is None:
+            qp, qs, qop, qos = None, 0, None, 0
+        else:
             raise ValueError("q_out without q")
-        sp, most = self._rows(rows, starts, max_tokens)
-        check(lib.sps_paged_append(self.handle, layer, kp, ks, vp, vs, None if rope is None else ctypes.byref(rope), qp,
-                                   qs, qop, qos, sp, rows, most, pos_offset, _raw_stream(dev)), "sps_paged_append")
+        if starts is None:
+            sp, most = None, rows // self.B if max_tokens is None else max_tokens
+        else:
+            sp = _flat(starts, dev, (self.B + 1,), torch.int32, "starts")
+            most = rows if max_tokens is None else max_tokens
+        st = lib.sps_paged_append(self.handle, layer, kp, ks, vp, vs, None if rope is None else ctypes.byref(rope), qp,
+                                  qs, qop, qos, sp, rows, most, pos_offset, _raw_stream(dev))
+        if st:
+            check(st, "sps_paged_append")
         return q_out
 
     def workspace(self, rows, max_tokens):
@@ -535,18 +552,24 @@ def paged_attention(kv, layer, q, ws, out=None, lse=None, starts=None, max_token
     over the positions up to its own, at most `window` of them (0: all). lse:
     fp32 [rows][n_heads] for the log of every row's sum. Rows as for append;
     scale defaults to head_dim ** -0.5."""
-    rows, H, D = q.shape[0], kv.n_heads, kv.head_dim
-    dev = _here(kv.buf, kv.dtype, "the cache")
-    qp, qs = _heads(q, rows, H, D, kv.dtype, "q")
+    rows, H, D, dt, dev = q.shape[0], kv.n_heads, kv.head_dim, kv.dtype, kv._device()
+    shape = (rows, H, D)
+    qp, qs = _heads(q, dev, shape, dt, "q")
     if out is None:
-        out = torch.empty((rows, H, D), dtype=kv.dtype, device=q.device)
-    op, os_ = _heads(out, rows, H, D, kv.dtype, "out")
-    lp = None if lse is None else _flat(lse, (rows, H), torch.float32, "lse")
-    sp, most = kv._rows(rows, starts, max_tokens)
-    _here(ws, torch.uint8, "the workspace")
-    check(lib.sps_paged_attention(kv.handle, layer, qp, qs, sp, rows, most, pos_offset,
-                                  D ** -0.5 if scale is None else scale, window, op, os_, lp, ws.data_ptr(),
-                                  ws.numel(), _raw_stream(dev)), "sps_paged_attention")
+        out = torch.empty(shape, dtype=dt, device=q.device)
+    op, os_ = _heads(out, dev, shape, dt, "out")
+    lp = None if lse is None else _flat(lse, dev, (rows, H), torch.float32, "lse")
+    if starts is None:
+        sp, most = None, rows // kv.B if max_tokens is None else max_tokens
+    else:
+        sp = _flat(starts, dev, (kv.B + 1,), torch.int32, "starts")
+        most = rows if max_tokens is None else max_tokens
+    n = ws.shape[0]
+    st = lib.sps_paged_attention(kv.handle, layer, qp, qs, sp, rows, most, pos_offset, D ** -0.5 if scale is None else scale,
+                                 window, op, os_, lp, _flat(ws, dev, (n,), torch.uint8, "the workspace"), n,
+                                 _raw_stream(dev))
+    if st:
+        check(st, "sps_paged_attention")
     return out
 
 
