@@ -49,7 +49,10 @@ __device__ __forceinline__ void fill_cs(const RopeArgs& r, int rows, P pos, floa
 
 // `rows` rows of `heads` heads rotated (sign -1: the transpose), x -> out,
 // which may be x: a thread reads both halves of its pairs before it writes them.
-template <typename T>
+// kBatch: the runs of a thread whose loads go out before the first is needed (a
+// full card of work-groups hides them by itself: rope of 8192 x 64 x 128 54 us
+// with 1, 58 with 4; append, with its LDS, 40 and 35).
+template <int kBatch, typename T>
 __device__ __forceinline__ void rotate_rows(const T* x, int64_t ldx, int rows, int heads, int DH, const RopeArgs& r,
                                             const float2* cs, float sign, T* out, int64_t ldo) {
   const int np = r.rot / 2;
@@ -62,38 +65,56 @@ __device__ __forceinline__ void rotate_rows(const T* x, int64_t ldx, int rows, i
     const int per = static_cast<int>(blockDim.x / static_cast<uint32_t>(units)), n = rows * heads;
     if (h0 >= per) return;
     const float inv = 1.f / heads;
-    for (int i = h0; i < n; i += per) {
-      const int row = static_cast<int>((i + 0.5f) * inv), h = i - row * heads;   // i < 2^17: exact
-      const T* src = x + row * ldx + h * DH;
-      T* dst = out + row * ldo + h * DH;
-      if (u >= pairs) {
-        const int d = r.rot + (u - pairs) * 8;
-        store8_any(dst + d, load8_any(src + d));
-      } else if (r.interleaved) {
-        const f32x8 a = load8_any(src + u * 8);
-        const float2* t = cs + row * np + u * 4;
+    const bool half = u < pairs && !r.interleaved;
+    const int d = u < pairs ? u * 8 : r.rot + (u - pairs) * 8;
+    for (int i0 = h0; i0 < n; i0 += per * kBatch) {
+      Frag<T> a[kBatch], b[kBatch];
+      int rows_at[kBatch];
+      int64_t at[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int i = i0 + j * per;
+        if (i >= n) break;
+        const int row = static_cast<int>((i + 0.5f) * inv), h = i - row * heads;   // i < 2^17: exact
+        rows_at[j] = row;
+        at[j] = row * ldo + h * DH;
+        const T* src = x + row * ldx + h * DH;
+        a[j] = load_frag_any(src + d);
+        if (half) b[j] = load_frag_any(src + np + d);
+      }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        if (i0 + j * per >= n) break;
+        T* dst = out + at[j];
+        if (u >= pairs) {
+          store8_any(dst + d, __builtin_convertvector(a[j].v, f32x8));
+          continue;
+        }
+        const f32x8 xa = __builtin_convertvector(a[j].v, f32x8);
         f32x8 y;
+        if (half) {
+          const f32x8 xb = __builtin_convertvector(b[j].v, f32x8);
+          const float2* t = cs + rows_at[j] * np + d;
+          f32x8 z;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 w = t[e];
-          const float sn = sign * w.y;
-          y[2 * e] = a[2 * e] * w.x - a[2 * e + 1] * sn;
-          y[2 * e + 1] = a[2 * e] * sn + a[2 * e + 1] * w.x;
-        }
-        store8_any(dst + u * 8, y);
-      } else {
-        const f32x8 a = load8_any(src + u * 8), b = load8_any(src + np + u * 8);
-        const float2* t = cs + row * np + u * 8;
-        f32x8 y, z;
+          for (int e = 0; e < 8; ++e) {
+            const float2 w = t[e];
+            const float sn = sign * w.y;
+            y[e] = xa[e] * w.x - xb[e] * sn;
+            z[e] = xa[e] * sn + xb[e] * w.x;
+          }
+          store8_any(dst + np + d, z);
+        } else {
+          const float2* t = cs + rows_at[j] * np + d / 2;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float2 w = t[e];
-          const float sn = sign * w.y;
-          y[e] = a[e] * w.x - b[e] * sn;
-          z[e] = a[e] * sn + b[e] * w.x;
+          for (int e = 0; e < 4; ++e) {
+            const float2 w = t[e];
+            const float sn = sign * w.y;
+            y[2 * e] = xa[2 * e] * w.x - xa[2 * e + 1] * sn;
+            y[2 * e + 1] = xa[2 * e] * sn + xa[2 * e + 1] * w.x;
+          }
         }
-        store8_any(dst + u * 8, y);
-        store8_any(dst + np + u * 8, z);
+        store8_any(dst + d, y);
       }
     }
     return;
@@ -128,7 +149,7 @@ __global__ __launch_bounds__(256) void rope_kernel(const T* x, int64_t ldx, cons
   const int h0 = blockIdx.y * head_group, nh = min(head_group, heads - h0);
   fill_cs(r, n, [&](int row) { return positions[row0 + row]; }, cs);
   __syncthreads();
-  rotate_rows(x + row0 * ldx + h0 * DH, ldx, n, nh, DH, r, cs, sign, out + row0 * ldo + h0 * DH, ldo);
+  rotate_rows<1>(x + row0 * ldx + h0 * DH, ldx, n, nh, DH, r, cs, sign, out + row0 * ldo + h0 * DH, ldo);
 }
 
 hipError_t launch_rope(int dtype, const void* x, int64_t ldx, const int32_t* positions, const RopeArgs& r, int rows,
@@ -203,19 +224,26 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedView c, PagedRow
       page = -1;
     }
   }
+  const int runs = DH / 8;                         // 8 or 16: at most two a thread in 32 rows
+  Frag<T> vr[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int i = threadIdx.x + j * 256, row = i / static_cast<uint32_t>(runs), d = (i - row * runs) * 8;
+    if (i < n * runs) vr[j] = load_frag_any(v + (row0 + row) * ldv + h * DH + d);
+  }
   if (c.B > 64) __syncthreads();                   // `words` have been read
   fill_cs(ra, n, [&](int row) { return s.p0 + j0 + row; }, cs);
   __syncthreads();
-  if (q)
-    rotate_rows(q + row0 * ldq + h * c.G * DH, ldq, n, c.G, DH, ra, cs, 1.f, qo + row0 * ldqo + h * c.G * DH, ldqo);
-  if (page < 0) return;
-  rotate_rows(k + row0 * ldk + h * DH, ldk, n, 1, DH, ra, cs, 1.f, sk, ld);
-  const int runs = DH / 8;                         // 8 or 16
-  for (int i = threadIdx.x; i < n * runs; i += blockDim.x) {
-    const int row = i / static_cast<uint32_t>(runs), d = (i - row * runs) * 8;
-    *reinterpret_cast<Frag<T>*>(sv + row * ld + d) = load_frag_any(v + (row0 + row) * ldv + h * DH + d);
+  if (page >= 0) rotate_rows<4>(k + row0 * ldk + h * DH, ldk, n, 1, DH, ra, cs, 1.f, sk, ld);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int i = threadIdx.x + j * 256, row = i / static_cast<uint32_t>(runs), d = (i - row * runs) * 8;
+    if (i < n * runs) *reinterpret_cast<Frag<T>*>(sv + row * ld + d) = vr[j];
   }
+  if (q)
+    rotate_rows<4>(q + row0 * ldq + h * c.G * DH, ldq, n, c.G, DH, ra, cs, 1.f, qo + row0 * ldqo + h * c.G * DH, ldqo);
   __syncthreads();
+  if (page < 0) return;
   const size_t area = static_cast<size_t>(DH) << c.page_log2;
   const int in = pos0 & ((1 << c.page_log2) - 1);
   const size_t base = (static_cast<size_t>(page) * c.H + h) * area + static_cast<size_t>(in) * DH;
