@@ -88,14 +88,12 @@ __device__ __forceinline__ int blocks_per_range(const PagedView& c, const Class&
   for (int b = 0; b < c.B; ++b) most = max(most, __builtin_amdgcn_readlane(blocks, b));
   const int per = max(kPagedMinBlocks, static_cast<int>((most + lane) / (lane + 1u)));
   const float inv = 1.f / per;
+  const float work = static_cast<float>(wave_sum_u64(static_cast<uint64_t>(tiles) * blocks));
   int items = 0;
-  float work = 0.f;
   for (int b = 0; b < c.B; ++b) {
     const int t = __builtin_amdgcn_readlane(tiles, b), n = __builtin_amdgcn_readlane(blocks, b) + per - 1;
-    int ranges = static_cast<int>(n * inv);        // n / per: at most one off
-    ranges += (ranges + 1) * per <= n ? 1 : ranges * per > n ? -1 : 0;
-    items += t * max(ranges, 1);
-    work += static_cast<float>(t) * (n - per + 1);
+    // n / per, exactly: n < 2^21, so that half a unit outweighs the rounding.
+    items += t * max(static_cast<int>((static_cast<float>(n) + 0.5f) * inv), 1);
   }
   const bool split = lane && per < most;
   const float own = static_cast<float>(k.own + (split ? k.split : 0));
@@ -204,14 +202,26 @@ template <> __device__ __forceinline__ bool nonfinite<float>(float x) {
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Scores (of 16 positions from pos0 on) at positions that a row does not see go to -Inf.
-__device__ __forceinline__ void mask_scores(int pos0, int qpos, int window, int end, int grp, f32x4& s) {
-  const int lo = window ? qpos - window : -1;
+// What a row sees of a block, in places of this lane's (place k: position pos0 +
+// 4 grp + k, of the block's 16-position tiles k = 16 pt + r): lo < k <= hi.
+struct Seen {
+  int lo, hi;
+};
+__device__ __forceinline__ Seen seen_of(int pos0, int qpos, int window, int end, int grp) {
+  const int at = pos0 + grp * 4;
+  return Seen{window ? qpos - window - at : -1 - at, min(qpos, end - 1) - at};
+}
+// The scores of a block at places that the row does not see go to -Inf.
+__device__ __forceinline__ void mask_scores(const Seen& v, bool windowed, f32x4 (&s)[2]) {
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int pos = pos0 + grp * 4 + r;
-    s[r] = pos <= qpos && pos > lo && pos < end ? s[r] : -INFINITY;
-  }
+  for (int pt = 0; pt < 2; ++pt)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s[pt][r] = pt * 16 + r <= v.hi ? s[pt][r] : -INFINITY;
+  if (!windowed) return;
+#pragma unroll
+  for (int pt = 0; pt < 2; ++pt)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s[pt][r] = pt * 16 + r > v.lo ? s[pt][r] : -INFINITY;
 }
 
 // Online softmax of one query row, spread over the four lanes with its column.
@@ -240,7 +250,20 @@ __device__ __forceinline__ float scale_scores(f32x4 (&s)[NP], float c_log2, cons
   }
   return mx;
 }
-// The same with a new reference where one is due; all QT rows of the lane
+// The first reference: nothing is summed yet, so nothing else changes.
+template <int NP>
+__device__ __forceinline__ void first_reference(f32x4 (&s)[NP], float mx, RowSoftmax& w) {
+  mx = fmaxf(mx, __shfl_xor(mx, 16));
+  mx = fmaxf(mx, __shfl_xor(mx, 32));
+  const bool some = mx > -INFINITY;
+  w.off = some ? mx : 0.f;
+  w.lim = some ? kLag : -INFINITY;
+#pragma unroll
+  for (int pt = 0; pt < NP; ++pt)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s[pt][r] -= w.off;
+}
+// scale_scores with a new reference where one is due; all QT rows of the lane
 // together, so that one branch skips the rescaling.
 template <int QT, int NP, int ND>
 __device__ __forceinline__ void softmax_scale(f32x4 (&s)[QT][NP], float c_log2, RowSoftmax (&w)[QT], f32x4 (&o)[QT][ND]) {
@@ -282,12 +305,26 @@ __device__ __forceinline__ void softmax_weights(f32x4 (&s)[NP], RowSoftmax& w) {
     }
 }
 
-// The values of positions past the last one, which may hold anything, cleared.
-template <typename T>
-__device__ __forceinline__ void clear_past(Frag<T>& vf, int pos0, int end, int grp) {
+// The values of positions past the last one, which may hold anything, cleared:
+// n fragments of a block, `left` positions of which are to be kept.
+template <typename T, int N>
+__device__ __forceinline__ void clear_past(Frag<T> (&vf)[N], int left, int grp) {
+  constexpr int kWords = 8 * sizeof(T) / 4, kPer = 4 / sizeof(T);   // 32-bit words of a fragment, elements of a word
+  typedef uint32_t words __attribute__((ext_vector_type(kWords)));
+  words keep;
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (pos0 + (e >> 2) * 16 + grp * 4 + (e & 3) >= end) vf.v[e] = from_f32<T>(0.f);
+  for (int i = 0; i < kWords; ++i) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const int x = i * kPer + e;
+      m |= (x >> 2) * 16 + (x & 3) < left - grp * 4 ? (kPer == 1 ? ~0u : 0xffffu << (16 * e)) : 0;
+    }
+    keep[i] = m;
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    vf[j].v = __builtin_bit_cast(decltype(vf[j].v), __builtin_bit_cast(words, vf[j].v) & keep);
 }
 
 // Values of a block in which some row of the tile does not see some position:
@@ -373,9 +410,9 @@ __device__ __forceinline__ void few_item(const PagedView& c, const Class& k, con
   const int r16 = lane & 15, grp = lane >> 4;
   const SeqRows& s = pl.s;
   const int cap = c.max_pages << c.page_log2;
-  const int nrows = s.n * c.G, row0 = 0;
-  // Positions of the tile's first and last token, and what they see.
-  const int first = s.p0 + uniform(row0 / c.G), last = s.p0 + uniform((nrows - 1) / c.G);
+  const int nrows = s.n * c.G;
+  // Positions of the first and last token, and what they see.
+  const int first = s.p0, last = s.p0 + s.n - 1;
   const int end = min(max(last + 1, 0), cap);
   const int lo = window ? min(max(first - window + 1, 0), end) : 0;
   const int base = (window ? min(max(s.p0 - window + 1, 0), min(max(s.p0 + s.n, 0), cap)) : 0) / 32;
@@ -386,18 +423,24 @@ __device__ __forceinline__ void few_item(const PagedView& c, const Class& k, con
   // or fp32) in LDS, where all waves read them: two waves per SIMD need the room.
   constexpr bool kStaged = QT > 1 || sizeof(T) == 4;
   Frag<T> qf[kStaged ? 1 : DH / 32];
-  int qpos[QT], tok[QT], head[QT];
+  // Token of row qt * 16 + r16 (-1: none): 64 rows at most, the quotient is exact.
+  const float inv_g = 1.f / c.G;
+  int in16 = r16;
+  auto token = [&](int qt) {
+    const int row = qt * 16 + in16;
+    return row < nrows ? static_cast<int>((row + 0.5f) * inv_g) : -1;
+  };
+  auto position = [&](int qt) {
+    const int t = token(qt);
+    return t < 0 ? -1 : s.p0 + t;
+  };
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {
-    const int row = row0 + qt * 16 + r16;
+    const int row = qt * 16 + r16, t = max(token(qt), 0);
     const bool valid = row < nrows;
-    const int t = valid ? row / c.G : 0;
-    tok[qt] = s.r0 + t;
-    head[qt] = pl.kvh * c.G + (valid ? row - t * c.G : 0);
-    qpos[qt] = valid ? s.p0 + t : -1;
 #pragma unroll
     for (int dt = 0; dt < DH / 32; ++dt) {
-      const T* src = q + tok[qt] * ldq + head[qt] * DH + dt * 32 + grp * 8;
+      const T* src = q + (s.r0 + t) * ldq + (pl.kvh * c.G + row - t * c.G) * DH + dt * 32 + grp * 8;
       if (!kStaged)
         qf[dt] = valid ? load_frag_any(src) : Frag<T>::zero();
       else if ((qt * (DH / 32) + dt) % 4 == wave)
@@ -481,22 +524,26 @@ __device__ __forceinline__ void few_item(const PagedView& c, const Class& k, con
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
       softmax_weights(sc[qt], w[qt]);
-      // bf16: the weights as hi + lo, p to 2^-16 relative; the second product
-      // costs nothing where the loads are what takes the time.
+      // The weights in bf16: with few rows as hi + lo, p to 2^-16 relative (the
+      // second product costs nothing where the loads are what takes the time),
+      // with three tiles, where registers are short, rounded once: half a step,
+      // 2^-8 of each, which averages out over a row like the values' own rounding.
+      constexpr bool kLow = QT < 3 && sizeof(T) == 2;
       Frag<T> hi, lw;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float p = sc[qt][e >> 2][e & 3];
         hi.v[e] = from_f32<T>(p);
-        lw.v[e] = from_f32<T>(p - to_f32(hi.v[e]));
+        if (kLow) lw.v[e] = from_f32<T>(p - to_f32(hi.v[e]));
       }
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) {
         o[qt][dt] = mma8(o[qt][dt], vf[dt], hi);
-        if (sizeof(T) == 2) o[qt][dt] = mma8(o[qt][dt], vf[dt], lw);
+        if (kLow) o[qt][dt] = mma8(o[qt][dt], vf[dt], lw);
       }
     }
   };
+  bool fresh = true;                               // no reference yet
   while (i < nb) {
     f32x4 sc[QT][2];
     // Blocks that every row sees all of and that need no new reference: nothing
@@ -506,9 +553,19 @@ __device__ __forceinline__ void few_item(const PagedView& c, const Class& k, con
       if (pos0 + 31 > min(first, end - 1) || (window && pos0 <= last - window)) break;
       scores(sc);
       bool up = false;
+      float mx[QT];
 #pragma unroll
-      for (int qt = 0; qt < QT; ++qt) up |= scale_scores(sc[qt], c_log2, w[qt]) > w[qt].lim;
-      if (__ballot(up)) break;
+      for (int qt = 0; qt < QT; ++qt) {
+        mx[qt] = scale_scores(sc[qt], c_log2, w[qt]);
+        up |= mx[qt] > w[qt].lim;
+      }
+      if (fresh) {
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) first_reference(sc[qt], mx[qt], w[qt]);
+        fresh = false;
+      } else if (__ballot(up)) {
+        break;
+      }
       const int next = seek(i + 1);
       if (next < nb) load_keys();
       products(sc);
@@ -517,26 +574,25 @@ __device__ __forceinline__ void few_item(const PagedView& c, const Class& k, con
       if (i >= nb) break;
     }
     if (i >= nb) break;
+    fresh = false;
     const int pos0 = (blk0 + wave + 4 * i) * 32;
     scores(sc);
     const bool masked = pos0 + 31 > min(first, end - 1) || (window && pos0 <= last - window);
     if (masked) {
 #pragma unroll
-      for (int qt = 0; qt < QT; ++qt)
-#pragma unroll
-        for (int pt = 0; pt < 2; ++pt) mask_scores(pos0 + pt * 16, qpos[qt], window, end, grp, sc[qt][pt]);
+      for (int qt = 0; qt < QT; ++qt) mask_scores(seen_of(pos0, position(qt), window, end, grp), window != 0, sc[qt]);
     }
     softmax_scale(sc, c_log2, w, o);
     if (masked) {
-      if (pos0 + 32 > end) {
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt) clear_past(vf[dt], pos0, end, grp);
-      }
+      if (pos0 + 32 > end) clear_past(vf, end - pos0, grp);
       // The values times zero: NaN if one of them is not finite.
       f32x4 zero{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) zero = mma8(zero, vf[dt], Frag<T>::zero());
       if (__ballot(zero[0] + zero[1] + zero[2] + zero[3] != 0.f)) {
+        int qpos[QT];
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) qpos[qt] = position(qt);
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) clean_values(vf[dt], pos0, qpos, window, end, grp, o, dt);
       }
@@ -549,6 +605,7 @@ __device__ __forceinline__ void few_item(const PagedView& c, const Class& k, con
     }
   }
 
+  asm volatile("" : "+v"(in16));                   // the rows' places again, not kept through the loop
   float ref[QT], sum[QT];
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {
@@ -578,9 +635,9 @@ __device__ __forceinline__ void few_item(const PagedView& c, const Class& k, con
 #pragma unroll
       for (int d = 0; d < ND / 4; ++d) part[d] += a * sm[(x * ND + wave * (ND / 4) + d) * 64 + lane];
     }
-    if (row0 + r16 < nrows)
-      write_row<T, DH, ND / 4>(c, k, pl, r16, tok[0], head[0], grp, wave * (ND / 4), m, l, part, out, ldo, lse, part_o,
-                               part_ml);
+    if (const int t = token(0); t >= 0)
+      write_row<T, DH, ND / 4>(c, k, pl, r16, s.r0 + t, pl.kvh * c.G + r16 - t * c.G, grp, wave * (ND / 4), m, l, part,
+                               out, ldo, lse, part_o, part_ml);
     return;
   }
   // Waves 2, 3 into 0, 1, then 1 into 0.
@@ -612,9 +669,9 @@ __device__ __forceinline__ void few_item(const PagedView& c, const Class& k, con
   if (wave) return;
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt)
-    if (row0 + qt * 16 + r16 < nrows)
-      write_row<T, DH, ND>(c, k, pl, qt * 16 + r16, tok[qt], head[qt], grp, 0, ref[qt], sum[qt], o[qt], out, ldo, lse,
-                           part_o, part_ml);
+    if (const int t = token(qt); t >= 0)
+      write_row<T, DH, ND>(c, k, pl, qt * 16 + r16, s.r0 + t, pl.kvh * c.G + qt * 16 + r16 - t * c.G, grp, 0, ref[qt],
+                           sum[qt], o[qt], out, ldo, lse, part_o, part_ml);
 }
 
 // The tiles an item has are its sequence's (k.tile holds all its rows): its own
@@ -729,14 +786,23 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
   const int wlast = wrow0 < nrows ? s.p0 + uniform((min(wrow0 + WR, nrows) - 1) / c.G) : -1;
   const float c_log2 = scale * 1.4426950408889634f;
 
+  // Token of the wave's row qt * 16 + r16 (-1: none), from that of its first.
+  const int tok0 = uniform(wrow0 / c.G), part0 = wrow0 - tok0 * c.G;
+  const float inv_g = 1.f / c.G;
+  auto token = [&](int qt) {
+    const int in = qt * 16 + r16;                  // part0 + in < G + 32: the quotient is exact
+    return wrow0 + in < nrows ? tok0 + static_cast<int>((part0 + in + 0.5f) * inv_g) : -1;
+  };
+  auto position = [&](int qt) {
+    const int t = token(qt);
+    return t < 0 ? -1 : s.p0 + t;
+  };
   Frag<T> qf[QT][DH / 32];
-  int qpos[QT];
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {
     const int row = wrow0 + qt * 16 + r16;
     const bool valid = row < nrows;
-    const int t = valid ? row / c.G : 0;
-    qpos[qt] = valid ? s.p0 + t : -1;
+    const int t = max(token(qt), 0);
     const T* src = q + (s.r0 + t) * ldq + (pl.kvh * c.G + (valid ? row - t * c.G : 0)) * DH + grp * 8;
 #pragma unroll
     for (int dt = 0; dt < DH / 32; ++dt) qf[qt][dt] = valid ? load_frag_any(src + dt * 32) : Frag<T>::zero();
@@ -884,9 +950,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
       scores(sc, b, h);
       if (masked) {
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt)
-#pragma unroll
-          for (int pt = 0; pt < 2; ++pt) mask_scores(pos0 + pt * 16, qpos[qt], window, end, grp, sc[qt][pt]);
+        for (int qt = 0; qt < QT; ++qt) mask_scores(seen_of(pos0, position(qt), window, end, grp), window != 0, sc[qt]);
       }
       softmax_scale(sc, c_log2, w, o);
       Frag<T> pf[QT];
@@ -914,14 +978,19 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
       } else {
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) {
-          Frag<T> vf = load_frag(&stage[b][h][1][(dt * 64 + lane) * 8]);
-          clear_past(vf, pos0, end, grp);
+          Frag<T> vf[1] = {load_frag(&stage[b][h][1][(dt * 64 + lane) * 8])};
+          if (pos0 + 32 > end) clear_past(vf, end - pos0, grp);
           bool odd = false;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) odd |= nonfinite(vf.v[e]);
-          if (__ballot(odd)) clean_values(vf, pos0, qpos, window, end, grp, o, dt);
+          for (int e = 0; e < 8; ++e) odd |= nonfinite(vf[0].v[e]);
+          if (__ballot(odd)) {
+            int qpos[QT];
 #pragma unroll
-          for (int qt = 0; qt < QT; ++qt) o[qt][dt] = mma8(o[qt][dt], vf, pf[qt]);
+            for (int qt = 0; qt < QT; ++qt) qpos[qt] = position(qt);
+            clean_values(vf[0], pos0, qpos, window, end, grp, o, dt);
+          }
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt) o[qt][dt] = mma8(o[qt][dt], vf[0], pf[qt]);
         }
       }
     }
@@ -936,7 +1005,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
     sum += __shfl_xor(sum, 32);
     const int row = wrow0 + qt * 16 + r16;
     if (row < nrows) {
-      const int t = row / c.G;
+      const int t = token(qt);
       write_row<T, DH, ND>(c, k, pl, row - row0, s.r0 + t, pl.kvh * c.G + row - t * c.G, grp, 0, w[qt].ref(), sum, o[qt],
                            out, ldo, lse, part_o, part_ml);
     }
