@@ -793,16 +793,14 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
     const int in = qt * 16 + r16;                  // part0 + in < G + 32: the quotient is exact
     return wrow0 + in < nrows ? tok0 + static_cast<int>((part0 + in + 0.5f) * inv_g) : -1;
   };
-  auto position = [&](int qt) {
-    const int t = token(qt);
-    return t < 0 ? -1 : s.p0 + t;
-  };
   Frag<T> qf[QT][DH / 32];
+  int qpos[QT];
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {
     const int row = wrow0 + qt * 16 + r16;
     const bool valid = row < nrows;
     const int t = max(token(qt), 0);
+    qpos[qt] = valid ? s.p0 + t : -1;
     const T* src = q + (s.r0 + t) * ldq + (pl.kvh * c.G + (valid ? row - t * c.G : 0)) * DH + grp * 8;
 #pragma unroll
     for (int dt = 0; dt < DH / 32; ++dt) qf[qt][dt] = valid ? load_frag_any(src + dt * 32) : Frag<T>::zero();
@@ -950,7 +948,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
       scores(sc, b, h);
       if (masked) {
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt) mask_scores(seen_of(pos0, position(qt), window, end, grp), window != 0, sc[qt]);
+        for (int qt = 0; qt < QT; ++qt) mask_scores(seen_of(pos0, qpos[qt], window, end, grp), window != 0, sc[qt]);
       }
       softmax_scale(sc, c_log2, w, o);
       Frag<T> pf[QT];
@@ -983,12 +981,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
           bool odd = false;
 #pragma unroll
           for (int e = 0; e < 8; ++e) odd |= nonfinite(vf[0].v[e]);
-          if (__ballot(odd)) {
-            int qpos[QT];
-#pragma unroll
-            for (int qt = 0; qt < QT; ++qt) qpos[qt] = position(qt);
-            clean_values(vf[0], pos0, qpos, window, end, grp, o, dt);
-          }
+          if (__ballot(odd)) clean_values(vf[0], pos0, qpos, window, end, grp, o, dt);
 #pragma unroll
           for (int qt = 0; qt < QT; ++qt) o[qt][dt] = mma8(o[qt][dt], vf[0], pf[qt]);
         }
