@@ -41,6 +41,7 @@ struct Place {
 // where it is one of several ranges split more for its partials.
 struct Class {
   int tile, target, above, limit, own, split;
+  int slots;               // the workspace's
 };
 
 // What the second launch has to join: entry i of the slots' descriptors, if i
@@ -185,11 +186,16 @@ __device__ __forceinline__ bool find_place(const PagedView& c, const PagedRows& 
   return found;
 }
 
-// A tile's first range leaves what the second launch needs, the others that there is nothing.
-__device__ __forceinline__ void leave_join(const PagedView& c, const Place& pl, Join* joins) {
-  if (threadIdx.x == 0 && pl.ranges > 1)
-    joins[pl.slot + static_cast<long>(pl.range) * c.H] =
-        Join{pl.s.r0, pl.s.n * c.G, pl.tile, pl.kvh, pl.range == 0 ? pl.ranges : 0};
+// A tile's first range leaves what the second launch needs, the others that
+// there is nothing. False: no slot for this item (only starts that break the
+// rules claim more rows than there are, and with them more slots).
+__device__ __forceinline__ bool leave_join(const PagedView& c, const Class& k, const Place& pl, Join* joins) {
+  if (pl.ranges == 1) return true;
+  const long slot = pl.slot + static_cast<long>(pl.range) * c.H, last = pl.slot + static_cast<long>(pl.ranges - 1) * c.H;
+  if (slot >= k.slots) return false;
+  if (threadIdx.x == 0)
+    joins[slot] = Join{pl.s.r0, pl.s.n * c.G, pl.tile, pl.kvh, pl.range == 0 && last < k.slots ? pl.ranges : 0};
+  return true;
 }
 
 template <typename T> __device__ __forceinline__ bool nonfinite(T x);  // Inf or NaN
@@ -685,7 +691,7 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedView c, PagedRow
   __shared__ FewLds<T, DH, QT> lds;
   Place pl;
   if (!find_place(c, r, window, k, reinterpret_cast<int*>(lds.o), count, err, &pl)) return;
-  leave_join(c, pl, joins);
+  if (!leave_join(c, k, pl, joins)) return;
   const int tiles = (pl.s.n * c.G + 15) / 16;
   if (tiles <= 1)
     few_item<T, DH, 1>(c, k, pl, q, ldq, scale, window, out, ldo, lse, part_o, part_ml, err, lds);
@@ -766,7 +772,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
   static_assert(sizeof(stage) >= 2 * kMaxPagedB * sizeof(int), "the plan's words");
   Place pl;
   if (!find_place(c, r, window, k, reinterpret_cast<int*>(stage), count, err, &pl)) return;
-  leave_join(c, pl, joins);
+  if (!leave_join(c, k, pl, joins)) return;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int r16 = lane & 15, grp = lane >> 4;
   const SeqRows& s = pl.s;
@@ -1021,7 +1027,8 @@ static hipError_t attn_t(const PagedView& c, const PagedRows& r, const PagedPlan
   const T* qq = static_cast<const T*>(q);
   T* oo = static_cast<T*>(out);
   // Blocks take about 1 us; an item's start 4 (8: its queries and first stage), a partial of 128 rows 20.
-  const Class few{p.few.tile, p.few.target, 0, p.limit, 4, p.qt}, many{p.many.tile, p.many.target, p.limit, INT32_MAX, 8, 20};
+  const Class few{p.few.tile, p.few.target, 0, p.limit, 4, p.qt, static_cast<int>(p.few.slots)};
+  const Class many{p.many.tile, p.many.target, p.limit, INT32_MAX, 8, 20, static_cast<int>(p.many.slots)};
   auto at = [&](size_t off) { return ws + off; };
   hipError_t e = hipSuccess;
   if (p.many.items) {

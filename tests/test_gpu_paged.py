@@ -230,6 +230,57 @@ def test_many_sequences(sps):
     t.check()
 
 
+def test_chunks_over_long_contexts_are_split(sps):
+    """Tiles of many rows with several ranges, joined; with a window, and among
+    more sequences than the ranges are priced for."""
+    for dtype, prior, new, window in (("bf16", [6000], [40], 0), ("bf16", [5000, 10], [33, 1], 3000),
+                                      ("f32", [3000], [20], 0), ("bf16", [4000] + [3] * 70, [70] + [1] * 70, 0)):
+        t = Batch(sps, dtype, 8, 2, 64, 64, prior, new, seed=19)
+        t.attend(window)
+        t.check(window)
+        again, al = t.out.clone(), t.lse.clone()
+        t.attend(window)
+        assert torch.equal(again, t.out) and torch.equal(al, t.lse)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_attention_of_drawn_batches(sps, seed):
+    g = np.random.default_rng(1000 + seed)
+    H = int(g.choice([1, 2, 3, 8]))
+    G = int(g.choice([1, 2, 3, 4, 5, 7, 8, 20]))
+    B = int(g.choice([1, 2, 5, 9, 70]))
+    D, page = int(g.choice([64, 128])), int(g.choice([32, 64, 128, 512]))
+    dtype = "f32" if g.random() < 0.3 else "bf16"
+    top = max(2, 600 // B)
+    prior = g.integers(0, top, B).tolist()
+    new = [int(g.choice([0, 1, 1, 2, 5, int(g.integers(1, 1 + max(1, 200 // B)))])) for _ in range(B)]
+    if sum(new) == 0:
+        new[0] = 1
+    window = int(g.choice([0, 0, 1, 31, 32, 33, 300]))
+    t = Batch(sps, dtype, H * G, H, D, page, prior, new, seed=seed, spare=1, extra_rows=int(g.integers(0, 3)))
+    # values of very unlike sizes, and keys that make some scores large
+    t.kv.buf[0, 1] *= torch.randn(t.kv.buf[0, 1].shape, device="cuda").exp().to(t.kv.dtype)
+    t.kv.buf[0, 0, ::3] *= 4
+    t.attend(window)
+    t.check(window)
+    assert sps.device_error() == 0
+
+
+def test_scores_that_grow_along_the_context(sps):
+    """Every few blocks a new largest score, far above the last (the reference
+    moves many times), and the same run backwards."""
+    for dtype, new in (("bf16", 1), ("bf16", 12), ("bf16", 80), ("f32", 3)):
+        t = Batch(sps, dtype, 4, 1, 64, 32, [700], [new], seed=23)
+        L = 700 + new
+        for grow in (np.linspace(0.0, 12.0, L), np.linspace(12.0, 0.0, L)):
+            d = np.arange(64)
+            for p in range(L):
+                t.kv.buf[0, 0, t.table[0, p // 32], 0, op.key_at(p % 32, d, 64)] = float(grow[p]) / 8
+            t.q.fill_(1.0)
+            t.attend(scale=1.0)
+            t.check(scale=1.0)
+
+
 def test_rows_outside_the_sequences_are_left(sps):
     t = Batch(sps, "bf16", 8, 2, 128, 64, [10, 400, 0], [2, 0, 70], seed=4, extra_rows=9, before=5)
     t.attend()
@@ -327,12 +378,31 @@ def test_starts_that_break_the_rules_are_flagged(sps):
     """Whatever they hold, nothing outside the rows and pages is touched and the flag is set."""
     t = Batch(sps, "bf16", 4, 2, 64, 32, [5, 40, 9], [4, 4, 4], seed=8)
     k, v = randn((12, 2, 64), 1, "bf16").cuda(), randn((12, 2, 64), 2, "bf16").cuda()
-    for starts in ([0, 4, 8, 13], [-1, 4, 8, 12], [0, 8, 4, 12], [0, 6, 8, 12], [0, 4, 8, 1 << 30]):
+    for starts in ([0, 4, 8, 13], [-1, 4, 8, 12], [0, 8, 4, 12], [0, 6, 8, 12], [0, 4, 8, 1 << 30], [8, 0, 12, 0],
+                   [-(1 << 31), (1 << 31) - 1, -(1 << 31), (1 << 31) - 1]):
         t.st = torch.tensor(starts, dtype=torch.int32, device="cuda")
         t.attend()
         assert sps.device_error() == sps.DEV_CAPACITY
         t.kv.append(0, k, v, starts=t.st, max_tokens=4)
         assert sps.device_error() == sps.DEV_CAPACITY
+
+
+def test_starts_that_claim_more_rows_than_there_are(sps):
+    """Overlapping claims of many sequences over split contexts: more items and
+    partials than the call's rows can have, which the workspace's end and the
+    memory behind the outputs do not feel."""
+    t = Batch(sps, "bf16", 4, 2, 64, 32, [2000] * 40, [1] * 40, seed=18)
+    # 30 tokens from position 2000 on reach a page that the tables do not have.
+    for most, flags in ((2, sps.DEV_CAPACITY), (30, sps.DEV_CAPACITY | sps.DEV_BAD_PAGE)):
+        rows = most
+        starts = [0, rows] * 20 + [0]
+        n = t.kv.workspace(rows, most).numel()
+        ws = torch.full((n + 4096,), 7, dtype=torch.uint8, device="cuda")
+        out = torch.full((rows + 2, 4, 64), 99.0, dtype=torch.bfloat16, device="cuda")
+        st = torch.tensor(starts, dtype=torch.int32, device="cuda")
+        sps.paged_attention(t.kv, 0, t.q[:rows], ws[:n], out=out[:rows], starts=st, max_tokens=most)
+        assert sps.device_error() == flags
+        assert bool((ws[n:] == 7).all()) and bool((out[rows:] == 99).all())
 
 
 # ---- append ------------------------------------------------------------------------
