@@ -752,8 +752,11 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedView c, int tile_r
 // second wave of every SIMD covers.
 __device__ __forceinline__ void copy_to_lds(const void* src, uint32_t lane_offset, uint32_t lds) {
   // Untracked by the compiler's wait counts: it would make every LDS read wait
-  // for the copies of the other stage too.
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_offset), "s"(src), "{m0}"(lds) : "memory");
+  // for the copies of the other stage too. Nor does it see that the address may
+  // come from v_readfirstlane right before, and a scalar register that a vector
+  // instruction wrote takes 5 wait states until a vector memory instruction may
+  // read it: s_nop 4 (M0 needs one of them).
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_offset), "s"(src), "{m0}"(lds) : "memory");
 }
 
 template <typename T, int DH, int QT, int NW>
