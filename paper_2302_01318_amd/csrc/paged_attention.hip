@@ -131,12 +131,12 @@ __device__ __forceinline__ int find_lane(int tiles, int blocks, int per, int wan
   return src;
 }
 
-// The place of item number blockIdx.x; false past the last. Every work-group
+// The place of item number idx; false past the last. Every work-group
 // computes the same plan from the same lengths; the first one leaves the number
 // of slots in *count. `words`: LDS for 2 kMaxPagedB ints, free again after the next barrier.
-__device__ __forceinline__ bool find_place(const PagedView& c, const PagedRows& r, int window, const Class& k, int* words,
-                                           int* count, int* err, Place* out) {
-  const int lane = threadIdx.x & 63, idx = blockIdx.x;
+__device__ __forceinline__ bool find_place(const PagedView& c, const PagedRows& r, int window, const Class& k, int idx,
+                                           int* words, int* count, int* err, Place* out) {
+  const int lane = threadIdx.x & 63;
   const int want = uniform(static_cast<int>(static_cast<uint32_t>(idx) / static_cast<uint32_t>(c.H)));
   const int kvh = idx - want * c.H;
   uint64_t before = 0;
@@ -530,11 +530,9 @@ __device__ __forceinline__ void few_item(const PagedView& c, const Class& k, con
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
       softmax_weights(sc[qt], w[qt]);
-      // The weights in bf16: with few rows as hi + lo, p to 2^-16 relative (the
-      // second product costs nothing where the loads are what takes the time),
-      // with three tiles, where registers are short, rounded once: half a step,
-      // 2^-8 of each, which averages out over a row like the values' own rounding.
-      constexpr bool kLow = QT < 3 && sizeof(T) == 2;
+      // The weights in bf16 as hi + lo, p to 2^-16 relative: the second product
+      // costs nothing where the loads are what takes the time.
+      constexpr bool kLow = sizeof(T) == 2;
       Frag<T> hi, lw;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -680,25 +678,39 @@ __device__ __forceinline__ void few_item(const PagedView& c, const Class& k, con
                            sum[qt], o[qt], out, ldo, lse, part_o, part_ml);
 }
 
-// The tiles an item has are its sequence's (k.tile holds all its rows): its own
-// straight code for each number of them, up to QT.
+// A class's share of the workspace.
+struct Parts {
+  float* o;
+  float2* ml;
+  Join* joins;
+  int* count;
+};
+
+// Item idx of the first class. The tiles it has are its sequence's (k.tile holds
+// all its rows): their own straight code for each number of them, up to QT.
+template <typename T, int DH, int QT>
+__device__ __forceinline__ void few_group(const PagedView& c, const PagedRows& r, const Class& k, int idx,
+                                          const T* __restrict__ q, int64_t ldq, float scale, int window,
+                                          T* __restrict__ out, int64_t ldo, float* __restrict__ lse, const Parts& w,
+                                          int* err, FewLds<T, DH, QT>& lds) {
+  Place pl;
+  if (!find_place(c, r, window, k, idx, reinterpret_cast<int*>(lds.o), w.count, err, &pl)) return;
+  if (!leave_join(c, k, pl, w.joins)) return;
+  const int tiles = (pl.s.n * c.G + 15) / 16;
+  if (tiles <= 1)
+    few_item<T, DH, 1>(c, k, pl, q, ldq, scale, window, out, ldo, lse, w.o, w.ml, err, lds);
+  else if (QT > 1 && (QT == 2 || tiles == 2))
+    few_item<T, DH, QT < 2 ? QT : 2>(c, k, pl, q, ldq, scale, window, out, ldo, lse, w.o, w.ml, err, lds);
+  else if (QT > 2)
+    few_item<T, DH, QT>(c, k, pl, q, ldq, scale, window, out, ldo, lse, w.o, w.ml, err, lds);
+}
+
 template <typename T, int DH, int QT>
 __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedView c, PagedRows r, Class k, const T* __restrict__ q,
                                                            int64_t ldq, float scale, int window, T* __restrict__ out,
-                                                           int64_t ldo, float* __restrict__ lse,
-                                                           float* __restrict__ part_o, float2* __restrict__ part_ml,
-                                                           Join* __restrict__ joins, int* __restrict__ count, int* err) {
+                                                           int64_t ldo, float* __restrict__ lse, Parts w, int* err) {
   __shared__ FewLds<T, DH, QT> lds;
-  Place pl;
-  if (!find_place(c, r, window, k, reinterpret_cast<int*>(lds.o), count, err, &pl)) return;
-  if (!leave_join(c, k, pl, joins)) return;
-  const int tiles = (pl.s.n * c.G + 15) / 16;
-  if (tiles <= 1)
-    few_item<T, DH, 1>(c, k, pl, q, ldq, scale, window, out, ldo, lse, part_o, part_ml, err, lds);
-  else if (QT > 1 && (QT == 2 || tiles == 2))
-    few_item<T, DH, QT < 2 ? QT : 2>(c, k, pl, q, ldq, scale, window, out, ldo, lse, part_o, part_ml, err, lds);
-  else if (QT > 2)
-    few_item<T, DH, QT>(c, k, pl, q, ldq, scale, window, out, ldo, lse, part_o, part_ml, err, lds);
+  few_group<T, DH, QT>(c, r, k, blockIdx.x, q, ldq, scale, window, out, ldo, lse, w, err, lds);
 }
 
 // The ranges of a tile's rows joined: 16 lanes per row, four rows per wave (one
@@ -759,23 +771,27 @@ __device__ __forceinline__ void copy_to_lds(const void* src, uint32_t lane_offse
   asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_offset), "s"(src), "{m0}"(lds) : "memory");
 }
 
+template <typename T, int DH>
+struct ManyLds {
+  static constexpr int NB = sizeof(T) == 2 ? 2 : 1;                // blocks per stage
+  static constexpr int kTile = 32 * DH;                            // elements of a block's keys or values
+  T stage[2][NB][2][kTile];
+  static_assert(2 * NB * 2 * kTile * sizeof(T) >= 2 * kMaxPagedB * sizeof(int), "the plan's words");
+};
+
 template <typename T, int DH, int QT, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, PagedRows r, Class k,
-                                                                const T* __restrict__ q, int64_t ldq, float scale,
-                                                                int window, T* __restrict__ out, int64_t ldo,
-                                                                float* __restrict__ lse, float* __restrict__ part_o,
-                                                                float2* __restrict__ part_ml, Join* __restrict__ joins,
-                                                                int* __restrict__ count, int* err) {
+__device__ __forceinline__ void many_group(const PagedView& c, const PagedRows& r, const Class& k, int idx,
+                                           const T* __restrict__ q, int64_t ldq, float scale, int window,
+                                           T* __restrict__ out, int64_t ldo, float* __restrict__ lse, const Parts& parts,
+                                           int* err, ManyLds<T, DH>& lds) {
   constexpr int ND = DH / 16, WR = 16 * QT;
-  constexpr int NB = sizeof(T) == 2 ? 2 : 1;                       // blocks per stage
-  constexpr int kTile = 32 * DH;                                   // elements of a block's keys or values
+  constexpr int NB = ManyLds<T, DH>::NB, kTile = ManyLds<T, DH>::kTile;
   constexpr int kCopies = kTile * static_cast<int>(sizeof(T)) / 1024;   // of one KiB
   static_assert(2 * NB * kCopies % NW == 0, "whole copies per wave");
-  __shared__ __align__(1024) T stage[2][NB][2][kTile];
-  static_assert(sizeof(stage) >= 2 * kMaxPagedB * sizeof(int), "the plan's words");
+  auto& stage = lds.stage;
   Place pl;
-  if (!find_place(c, r, window, k, reinterpret_cast<int*>(stage), count, err, &pl)) return;
-  if (!leave_join(c, k, pl, joins)) return;
+  if (!find_place(c, r, window, k, idx, reinterpret_cast<int*>(stage), parts.count, err, &pl)) return;
+  if (!leave_join(c, k, pl, parts.joins)) return;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int r16 = lane & 15, grp = lane >> 4;
   const SeqRows& s = pl.s;
@@ -1009,16 +1025,42 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_many_kernel(PagedView c, Pag
     if (row < nrows) {
       const int t = token(qt);
       write_row<T, DH, ND>(c, k, pl, row - row0, s.r0 + t, pl.kvh * c.G + row - t * c.G, grp, 0, w[qt].ref(), sum, o[qt],
-                           out, ldo, lse, part_o, part_ml);
+                           out, ldo, lse, parts.o, parts.ml);
     }
   }
 }
 
-// Three tiles are for bf16 alone (paged_few_tiles).
+template <typename T> constexpr int many_qt() { return sizeof(T) == 2 ? 2 : 1; }
+template <typename T> constexpr int many_waves() { return kManyTile / (16 * many_qt<T>()); }
+
 template <typename T, int DH>
-static auto few_kernel_3() {
-  if constexpr (sizeof(T) == 2) return paged_few_kernel<T, DH, 3>;
-  else return paged_few_kernel<T, DH, 2>;
+__global__ __launch_bounds__(64 * many_waves<T>(), 2) void paged_many_kernel(PagedView c, PagedRows r, Class k,
+                                                                            const T* __restrict__ q, int64_t ldq,
+                                                                            float scale, int window,
+                                                                            T* __restrict__ out, int64_t ldo,
+                                                                            float* __restrict__ lse, Parts w, int* err) {
+  __shared__ __align__(1024) ManyLds<T, DH> lds;
+  many_group<T, DH, many_qt<T>(), many_waves<T>()>(c, r, k, blockIdx.x, q, ldq, scale, window, out, ldo, lse, w, err, lds);
+}
+
+// Both classes in one launch (bf16: both have four waves): the few rows' items,
+// which wait for memory, fill the CUs that the last tiles leave (a mixed batch
+// of 27 sequences 338 -> XX us).
+template <typename T, int DH>
+__global__ __launch_bounds__(256, 2) void paged_both_kernel(PagedView c, PagedRows r, Class many, int many_items,
+                                                            Class few, const T* __restrict__ q, int64_t ldq, float scale,
+                                                            int window, T* __restrict__ out, int64_t ldo,
+                                                            float* __restrict__ lse, Parts wm, Parts wf, int* err) {
+  constexpr int QT = paged_few_tiles(SPS_DTYPE_BF16);
+  constexpr size_t kBytes = sizeof(ManyLds<T, DH>) > sizeof(FewLds<T, DH, QT>) ? sizeof(ManyLds<T, DH>)
+                                                                                : sizeof(FewLds<T, DH, QT>);
+  __shared__ __align__(1024) char lds[kBytes];
+  if (static_cast<int>(blockIdx.x) < many_items)
+    many_group<T, DH, many_qt<T>(), many_waves<T>()>(c, r, many, blockIdx.x, q, ldq, scale, window, out, ldo, lse, wm, err,
+                                                     reinterpret_cast<ManyLds<T, DH>&>(lds));
+  else
+    few_group<T, DH, QT>(c, r, few, blockIdx.x - many_items, q, ldq, scale, window, out, ldo, lse, wf, err,
+                         reinterpret_cast<FewLds<T, DH, QT>&>(lds));
 }
 
 static_assert(sizeof(Join) == kPagedJoinBytes, "the workspace's entries");
@@ -1032,30 +1074,37 @@ static hipError_t attn_t(const PagedView& c, const PagedRows& r, const PagedPlan
   // Blocks take about 1 us; an item's start 4 (8: its queries and first stage), a partial of 128 rows 20.
   const Class few{p.few.tile, p.few.target, 0, p.limit, 4, p.qt, static_cast<int>(p.few.slots)};
   const Class many{p.many.tile, p.many.target, p.limit, INT32_MAX, 8, 20, static_cast<int>(p.many.slots)};
-  auto at = [&](size_t off) { return ws + off; };
+  auto parts = [&](const PagedClass& k) {
+    return Parts{reinterpret_cast<float*>(ws + k.o_off), reinterpret_cast<float2*>(ws + k.ml_off),
+                 reinterpret_cast<Join*>(ws + k.join_off), reinterpret_cast<int*>(ws + k.count_off)};
+  };
+  const Parts wf = parts(p.few), wm = parts(p.many);
+  const dim3 gf(static_cast<unsigned>(p.few.items)), gm(static_cast<unsigned>(p.many.items));
   hipError_t e = hipSuccess;
-  if (p.many.items) {
-    constexpr int kQt = sizeof(T) == 2 ? 2 : 1, kWaves = kManyTile / (16 * kQt);
-    hipLaunchKernelGGL((paged_many_kernel<T, DH, kQt, kWaves>), dim3(static_cast<unsigned>(p.many.items)),
-                       dim3(64 * kWaves), 0, st, c, r, many, qq, ldq, scale, window, oo, ldo, lse,
-                       reinterpret_cast<float*>(at(p.many.o_off)), reinterpret_cast<float2*>(at(p.many.ml_off)),
-                       reinterpret_cast<Join*>(at(p.many.join_off)), reinterpret_cast<int*>(at(p.many.count_off)), err);
+  if (sizeof(T) == 2 && p.many.items && p.few.items) {
+    if constexpr (sizeof(T) == 2)
+      hipLaunchKernelGGL((paged_both_kernel<T, DH>), dim3(gm.x + gf.x), dim3(256), 0, st, c, r, many,
+                         static_cast<int>(gm.x), few, qq, ldq, scale, window, oo, ldo, lse, wm, wf, err);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  if (p.few.items) {
-    auto kern = p.qt == 1 ? paged_few_kernel<T, DH, 1> : p.qt == 2 ? paged_few_kernel<T, DH, 2> : few_kernel_3<T, DH>();
-    hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(p.few.items)), dim3(256), 0, st, c, r, few, qq, ldq, scale,
-                       window, oo, ldo, lse, reinterpret_cast<float*>(at(p.few.o_off)),
-                       reinterpret_cast<float2*>(at(p.few.ml_off)), reinterpret_cast<Join*>(at(p.few.join_off)),
-                       reinterpret_cast<int*>(at(p.few.count_off)), err);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+  } else {
+    if (p.many.items) {
+      hipLaunchKernelGGL((paged_many_kernel<T, DH>), gm, dim3(64 * many_waves<T>()), 0, st, c, r, many, qq, ldq, scale,
+                         window, oo, ldo, lse, wm, err);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (p.few.items) {
+      // Three tiles are for bf16 alone (paged_few_tiles).
+      auto kern = p.qt == 1 ? paged_few_kernel<T, DH, 1> : p.qt == 2 || sizeof(T) == 4 ? paged_few_kernel<T, DH, 2>
+                                                                                      : paged_few_kernel<T, DH, sizeof(T) == 2 ? 3 : 2>;
+      hipLaunchKernelGGL(kern, gf, dim3(256), 0, st, c, r, few, qq, ldq, scale, window, oo, ldo, lse, wf, err);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
   }
   for (const PagedClass* k : {&p.many, &p.few}) {
     if (!k->slots) continue;
-    hipLaunchKernelGGL((paged_join_kernel<T, DH>), dim3(static_cast<unsigned>(k->slots), k->tile / 16),
-                       dim3(256), 0, st, c, k->tile, reinterpret_cast<const Join*>(at(k->join_off)),
-                       reinterpret_cast<const int*>(at(k->count_off)), reinterpret_cast<const float*>(at(k->o_off)),
-                       reinterpret_cast<const float2*>(at(k->ml_off)), oo, ldo, lse);
+    const Parts w = parts(*k);
+    hipLaunchKernelGGL((paged_join_kernel<T, DH>), dim3(static_cast<unsigned>(k->slots), k->tile / 16), dim3(256), 0, st, c,
+                       k->tile, w.joins, w.count, w.o, w.ml, oo, ldo, lse);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   return e;
