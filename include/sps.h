@@ -396,8 +396,8 @@ typedef struct sps_paged_s* sps_paged_t;
 size_t sps_paged_bytes(const sps_paged_config* cfg);
 
 /* Create a handle over `buf` (sps_paged_bytes bytes, 256-byte aligned),
- * `page_table` (device int32 [B][max_pages]; entries that no position below
- * a sequence's length needs are not read) and `lengths` (device int32 [B],
+ * `page_table` (device int32 [B][max_pages]; entries of pages in which a call
+ * neither writes nor sees a position are not read) and `lengths` (device int32 [B],
  * committed lengths, as for sps_kv_create, whose array it may be). The caller
  * initialises and updates both arrays. SPS_E_SHAPE for an invalid cfg. */
 sps_status sps_paged_create(const sps_paged_config* cfg, void* buf, const int32_t* page_table,
@@ -412,7 +412,8 @@ void sps_paged_destroy(sps_paged_t kv);
  * starts == NULL rows b max_tokens .. (b + 1) max_tokens - 1, and rows is B
  * max_tokens. Row j of its sequence sits at position lengths[b] + pos_offset + j;
  * lengths are not advanced. Starts that break these rules set
- * SPS_DEV_CAPACITY, and what the rows of their sequences get is not defined.
+ * SPS_DEV_CAPACITY, and what the call's rows get is not defined (nothing
+ * outside the rows and the tables' pages is written).
  * rows <= 2^20; strides are elements from row to row. */
 
 /* Write the new tokens' keys and values ([rows][n_kv_heads][head_dim], the

@@ -93,7 +93,7 @@ RopeArgs rope_args(const sps_rope_spec* r, int DH);   // NULL: no rotation
 hipError_t launch_rope(int dtype, const void* x, int64_t ldx, const int32_t* positions, const RopeArgs& r, int rows,
                        int heads, int DH, bool backward, void* out, int64_t ldo, hipStream_t st);
 
-// The paged cache (paged.hip, paged_attention.hip): one layer's planes and
+// The paged cache (rope.hip, paged_attention.hip): one layer's planes and
 // what finds a position in them, and the rows of a call (see sps.h).
 struct PagedView {
   void *k, *v;

@@ -24,10 +24,6 @@ __device__ __forceinline__ void store8_any(bf16* p, f32x8 v) {
   *reinterpret_cast<bf16x8u*>(p) = __builtin_convertvector(v, bf16x8u);
 }
 __device__ __forceinline__ void store8_any(float* p, f32x8 v) { *reinterpret_cast<f32x8u*>(p) = v; }
-__device__ __forceinline__ f32x8 load8_any(const bf16* p) {
-  return __builtin_convertvector(*reinterpret_cast<const bf16x8u*>(p), f32x8);
-}
-__device__ __forceinline__ f32x8 load8_any(const float* p) { return *reinterpret_cast<const f32x8u*>(p); }
 __device__ __forceinline__ void store4_any(bf16* p, f32x4 v) {
   *reinterpret_cast<bf16x4u*>(p) = __builtin_convertvector(v, bf16x4u);
 }

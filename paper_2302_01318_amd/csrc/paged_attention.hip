@@ -41,7 +41,7 @@ struct Place {
 // where it is one of several ranges split more for its partials.
 struct Class {
   int tile, target, above, limit, own, split;
-  int slots;               // the workspace's
+  int items, slots;        // the grid's, the workspace's
 };
 
 // What the second launch has to join: entry i of the slots' descriptors, if i
@@ -182,7 +182,10 @@ __device__ __forceinline__ bool find_place(const PagedView& c, const PagedRows& 
       found = true;
     }
   }
-  if (idx == 0 && threadIdx.x == 0) *count = static_cast<int>(static_cast<uint32_t>(before)) * c.H;
+  // More items than the grid has (only starts that break the rules): not every
+  // slot's descriptor is written, so that nothing is joined.
+  if (idx == 0 && threadIdx.x == 0)
+    *count = static_cast<int64_t>(before >> 32) * c.H <= k.items ? static_cast<int>(static_cast<uint32_t>(before)) * c.H : 0;
   return found;
 }
 
@@ -1072,8 +1075,10 @@ static hipError_t attn_t(const PagedView& c, const PagedRows& r, const PagedPlan
   const T* qq = static_cast<const T*>(q);
   T* oo = static_cast<T*>(out);
   // Blocks take about 1 us; an item's start 4 (8: its queries and first stage), a partial of 128 rows 20.
-  const Class few{p.few.tile, p.few.target, 0, p.limit, 4, p.qt, static_cast<int>(p.few.slots)};
-  const Class many{p.many.tile, p.many.target, p.limit, INT32_MAX, 8, 20, static_cast<int>(p.many.slots)};
+  const Class few{p.few.tile, p.few.target, 0, p.limit, 4, p.qt, static_cast<int>(p.few.items),
+                  static_cast<int>(p.few.slots)};
+  const Class many{p.many.tile, p.many.target, p.limit, INT32_MAX, 8, 20, static_cast<int>(p.many.items),
+                   static_cast<int>(p.many.slots)};
   auto parts = [&](const PagedClass& k) {
     return Parts{reinterpret_cast<float*>(ws + k.o_off), reinterpret_cast<float2*>(ws + k.ml_off),
                  reinterpret_cast<Join*>(ws + k.join_off), reinterpret_cast<int*>(ws + k.count_off)};

@@ -713,8 +713,11 @@ sps_status sps_paged_attention(sps_paged_t kv, int32_t layer, const void* q, int
   if (!good_stride(q_stride, qw) || !good_stride(out_stride, qw)) return SPS_E_INVALID;
   if (rows == 0) return SPS_OK;
   if (!q || !out || q == out || !workspace || misaligned(q, c.dtype) || misaligned(out, c.dtype) ||
-      reinterpret_cast<uintptr_t>(workspace) % 256)
+      misaligned(lse, SPS_DTYPE_F32) || reinterpret_cast<uintptr_t>(workspace) % 256)
     return SPS_E_INVALID;
+  // A window past every position (2^24 and a chunk, paged.h) is all of them:
+  // the kernels' differences then stay inside 32 bits.
+  window = std::min(window, 1 << 25);
   const sps::PagedPlan p = sps::paged_plan(c, starts != nullptr, rows, max_tokens);
   if (ws_bytes < p.total) return SPS_E_CAPACITY;
   int* err = device_error_ptr();

@@ -405,6 +405,35 @@ def test_starts_that_claim_more_rows_than_there_are(sps):
         assert bool((ws[n:] == 7).all()) and bool((out[rows:] == 99).all())
 
 
+def test_claims_of_short_sequences_before_long_ones(sps):
+    """Overlapping claims of which the first are not split: partials whose items
+    the call does not have are not joined, whatever the workspace holds."""
+    for dtype, B in (("bf16", 40), ("f32", 40), ("bf16", 100)):
+        t = Batch(sps, dtype, 4, 2, 64, 32, [40] * (B // 2) + [2000] * (B // 2), [1] * B, seed=19)
+        n = t.kv.workspace(1, 1).numel()
+        ws = torch.full((n + 4096,), 0x7f, dtype=torch.uint8, device="cuda")
+        out = torch.full((9, 4, 64), 99.0, dtype=DT[dtype], device="cuda")
+        lse = torch.full((9, 4), 99.0, device="cuda")
+        st = torch.tensor([0, 1] * (B // 2) + [0], dtype=torch.int32, device="cuda")
+        sps.paged_attention(t.kv, 0, t.q[:1], ws[:n], out=out[:1], lse=lse[:1], starts=st, max_tokens=1)
+        assert sps.device_error() == sps.DEV_CAPACITY
+        assert bool((ws[n:] == 0x7f).all()) and bool((out[1:] == 99).all()) and bool((lse[1:] == 99).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_windows_wider_than_any_context(sps, dtype):
+    """The widest window is no window, also for rows before position 0."""
+    for prior, new in (([-5, 40], [10, 3]), ([-70, 300], [150, 2])):
+        t = Batch(sps, dtype, 4, 2, 64, 32, [max(p, 0) for p in prior], new, seed=20)
+        t.prior = prior
+        t.kv.lengths.copy_(torch.tensor(prior, dtype=torch.int32))
+        t.attend(2147483647)
+        t.check()
+        wide = t.out.clone()
+        t.attend(0)
+        assert torch.equal(wide, t.out)
+
+
 # ---- append ------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("D, hq, hkv, page, prior, new", [

@@ -131,6 +131,11 @@ def test_attention_refuses(sps, handle, change, status):
                                        None) == status
 
 
+def test_attention_refuses_a_misaligned_lse(sps, handle):
+    assert sps.lib.sps_paged_attention(handle, 0, A, 1024, None, 6, 2, 0, 0.1, 0, P(1 << 20), 1024, P(4098), P(1 << 21),
+                                       1 << 30, None) == 1
+
+
 def test_no_rows_are_accepted(sps, handle):
     assert sps.lib.sps_paged_append(handle, 0, None, 256, None, 256, None, None, 0, None, 0, A, 0, 0, 0, None) == 0
     assert sps.lib.sps_paged_attention(handle, 0, None, 1024, A, 0, 0, 0, 1.0, 0, None, 1024, None, None, 0, None) == 0
