@@ -97,44 +97,67 @@ __device__ __forceinline__ float wave_min_dpp(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 
-// Blocks per range, by up to 64 sequences' tiles and blocks (one a lane): lane
-// r - 1 prices r ranges of the longest, in the time of a block: the rounds that
-// the items take over the card's `target` slots, or where sizes or rounds are
-// uneven the work per slot and most of an item until the last one ends
-// (work-groups go faster as others end). Joining costs kJoinBlocks. Every lane
-// takes the cheapest.
+// How the positions are split: the first `whole` tiles (of the sequences in
+// order) not at all, the others in ranges of `per` blocks.
+struct Split {
+  int whole, per;
+};
+
+// The split of up to 64 sequences' tiles and blocks (one a lane), priced in the
+// time of a block: lane r - 1 has r ranges of the longest, over the rounds that
+// the items take on the card's `target` slots, or where sizes or rounds are
+// uneven over the work per slot and most of an item until the last one ends
+// (work-groups go faster as others end). Where the tiles fill a round by
+// themselves the upper 32 lanes leave whole rounds unsplit and split what is
+// left (64 heads on 8, chunks of 1100 tokens at position 12000: 665 us with all
+// tiles alike, 469 so; 2300 at 8000 764 and 715). Joining costs kJoinBlocks.
+// Every lane takes the cheapest.
 constexpr int kJoinBlocks = 3;
-__device__ __forceinline__ int blocks_per_range(const PagedView& c, const Class& k, int tiles, int blocks) {
+__device__ __forceinline__ Split choose_split(const PagedView& c, const Class& k, int tiles, int blocks) {
   const int lane = threadIdx.x & 63;
-  int most = 0;
-  for (int b = 0; b < c.B; ++b) most = max(most, __builtin_amdgcn_readlane(blocks, b));
-  const int per = max(kPagedMinBlocks, static_cast<int>((most + lane) / (lane + 1u)));
-  const float inv = 1.f / per;
-  const float work = static_cast<float>(wave_sum_u64(static_cast<uint64_t>(tiles) * blocks));
-  int items = 0;
+  int most = 0, all = 0;
   for (int b = 0; b < c.B; ++b) {
-    const int t = __builtin_amdgcn_readlane(tiles, b), n = __builtin_amdgcn_readlane(blocks, b) + per - 1;
-    // n / per, exactly: n < 2^21, so that half a unit outweighs the rounding.
-    items += t * max(static_cast<int>((static_cast<float>(n) + 0.5f) * inv), 1);
+    most = max(most, __builtin_amdgcn_readlane(blocks, b));
+    all += __builtin_amdgcn_readlane(tiles, b);
   }
-  const bool split = lane && per < most;
+  const float slots = static_cast<float>(k.target);
+  const int rounds = static_cast<int>(static_cast<float>(all) * c.H / slots);
+  const bool rest = rounds && lane >= 32;
+  const int whole = rest ? rounds * k.target / c.H : 0, parts = rest ? lane - 30 : lane + 1;
+  const int per = max(kPagedMinBlocks, static_cast<int>((most + parts - 1u) / static_cast<uint32_t>(parts)));
+  const float inv = 1.f / per;
+  int items = 0, before = 0;
+  float work = 0.f;
+  for (int b = 0; b < c.B; ++b) {
+    const int t = __builtin_amdgcn_readlane(tiles, b), n = __builtin_amdgcn_readlane(blocks, b);
+    const int left = min(max(before + t - whole, 0), t);
+    before += t;
+    // (n + per - 1) / per, exactly: n < 2^17, so that half a unit outweighs the rounding.
+    items += left * max(static_cast<int>((static_cast<float>(n + per - 1) + 0.5f) * inv), 1);
+    work += static_cast<float>(left) * n;
+  }
+  const bool split = parts > 1 && per < most;
   const float own = static_cast<float>(k.own + (split ? k.split : 0));
-  const float n = static_cast<float>(items) * c.H, slots = static_cast<float>(k.target);
+  const float n = static_cast<float>(items) * c.H;
   const float each = min(per, most) + own;
-  float cost = fminf(ceilf(n / slots) * each, (work * c.H + n * own) / fminf(n, slots) + 0.75f * each);
+  float cost = n > 0.f ? fminf(ceilf(n / slots) * each, (work * c.H + n * own) / fminf(n, slots) + 0.75f * each) : 0.f;
   if (split) cost += kJoinBlocks;
-  if (lane && n > kPagedMostItems * slots) cost = INFINITY;        // the workspace's bound
+  if (rest) cost += rounds * static_cast<float>(most + k.own);
+  if (lane && n > (rest ? 1 : kPagedMostItems) * slots) cost = INFINITY;   // the grid's and the workspace's bound
   const uint64_t cheapest = __ballot(cost == wave_min_dpp(cost));
-  return cheapest ? __builtin_amdgcn_readlane(per, __ffsll(static_cast<unsigned long long>(cheapest)) - 1) : kPagedMinBlocks;
+  if (!cheapest) return Split{0, kPagedMinBlocks};
+  const int src = __ffsll(static_cast<unsigned long long>(cheapest)) - 1;
+  return Split{__builtin_amdgcn_readlane(whole, src), __builtin_amdgcn_readlane(per, src)};
 }
 
 // One step of the search for item `want` (of H KV heads each): `tiles` and
-// `blocks` of 64 sequences, one a lane; *before: (items << 32 | slots) of the
-// sequences before them. The lane that has it, or -1.
-__device__ __forceinline__ int find_lane(int tiles, int blocks, int per, int want, int kvh, int H, uint64_t* before,
-                                         Place* out) {
-  const uint32_t ranges = max(1u, (blocks + per - 1u) / per);
-  const uint32_t slots = ranges > 1 ? tiles * ranges : 0, mine = tiles * ranges;
+// `blocks` of 64 sequences, one a lane, the first `whole` of a lane's tiles
+// unsplit; *before: (items << 32 | slots) of the sequences before them. The lane
+// that has it, or -1.
+__device__ __forceinline__ int find_lane(int tiles, int blocks, int whole, int per, int want, int kvh, int H,
+                                         uint64_t* before, Place* out) {
+  const uint32_t ranges = max(1u, (blocks + per - 1u) / per), cut = (tiles - whole) * ranges;
+  const uint32_t slots = ranges > 1 ? cut : 0, mine = whole + cut;
   const uint64_t incl = wave_incl_scan_u64(static_cast<uint64_t>(mine) << 32 | slots) + *before;
   const uint64_t hit = __ballot(want < static_cast<int>(incl >> 32));
   *before = readlane_u64(incl, 63);
@@ -142,13 +165,23 @@ __device__ __forceinline__ int find_lane(int tiles, int blocks, int per, int wan
   const int src = __ffsll(static_cast<unsigned long long>(hit)) - 1;
   const uint64_t inc = readlane_u64(incl, src);
   const int at = want - (static_cast<int>(inc >> 32) - __builtin_amdgcn_readlane(static_cast<int>(mine), src));
-  out->ranges = __builtin_amdgcn_readlane(static_cast<int>(ranges), src);
-  out->tile = uniform(static_cast<int>(static_cast<uint32_t>(at) / static_cast<uint32_t>(out->ranges)));
-  out->range = at - out->tile * out->ranges;
+  const int first = __builtin_amdgcn_readlane(whole, src);
   out->kvh = kvh;
+  if (at < first) {
+    out->ranges = 1;
+    out->tile = at;
+    out->range = 0;
+    out->per = 1 << 20;                            // all blocks
+    out->slot = 0;
+    return src;
+  }
+  out->ranges = __builtin_amdgcn_readlane(static_cast<int>(ranges), src);
+  const int tile = uniform(static_cast<int>(static_cast<uint32_t>(at - first) / static_cast<uint32_t>(out->ranges)));
+  out->tile = first + tile;
+  out->range = at - first - tile * out->ranges;
   out->per = per;
   const uint32_t slot0 = static_cast<uint32_t>(inc) - __builtin_amdgcn_readlane(static_cast<int>(slots), src);
-  out->slot = (static_cast<long>(slot0) + static_cast<long>(out->tile) * out->ranges) * H + kvh;
+  out->slot = (static_cast<long>(slot0) + static_cast<long>(tile) * out->ranges) * H + kvh;
   return src;
 }
 
@@ -168,8 +201,13 @@ __device__ __forceinline__ bool find_place(const PagedView& c, const PagedRows& 
     if (lane < c.B) s = seq_rows(c, r, lane);
     if (idx == 0 && s.bad) atomicOr(err, kErrCapacity);
     const int2 tb = lane < c.B ? tiles_blocks(c, k, s, window) : make_int2(0, 0);
-    const int per = blocks_per_range(c, k, tb.x, tb.x ? tb.y : 0);
-    const int src = find_lane(tb.x, tb.y, per, want, kvh, c.H, &before, out);
+    const Split sp = choose_split(c, k, tb.x, tb.x ? tb.y : 0);
+    int whole = 0;
+    if (sp.whole) {
+      const int end = static_cast<int>(wave_incl_scan_u64(static_cast<uint64_t>(tb.x)));
+      whole = tb.x - min(max(end - sp.whole, 0), tb.x);
+    }
+    const int src = find_lane(tb.x, tb.y, whole, sp.per, want, kvh, c.H, &before, out);
     if (src >= 0) {
       out->b = src;
       out->s.r0 = __builtin_amdgcn_readlane(s.r0, src);
@@ -195,7 +233,8 @@ __device__ __forceinline__ bool find_place(const PagedView& c, const PagedRows& 
     for (int b0 = 0; b0 < c.B && (!found || idx == 0); b0 += 64) {
       Place here;
       const int b = b0 + lane;
-      const int src = find_lane(b < c.B ? s_tiles[b] : 0, b < c.B ? s_blocks[b] : 0, per, want, kvh, c.H, &before, &here);
+      const int src = find_lane(b < c.B ? s_tiles[b] : 0, b < c.B ? s_blocks[b] : 0, 0, per, want, kvh, c.H,
+                                &before, &here);
       if (src < 0 || found) continue;
       *out = here;
       out->b = uniform(b0 + src);
@@ -820,14 +859,14 @@ __device__ __forceinline__ void many_group(const PagedView& c, const PagedRows& 
   auto& stage = lds.stage;
   Place pl;
   if (!find_place(c, r, window, k, idx, reinterpret_cast<int*>(stage), parts.count, err, &pl)) return;
+  // The last tiles of a prompt see most: they go first.
+  const int nrows = pl.s.n * c.G, ntiles = uniform((nrows + k.tile - 1) / k.tile), tile = ntiles - 1 - pl.tile;
+  pl.tile = tile;
   if (!leave_join(c, k, pl, parts.joins)) return;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int r16 = lane & 15, grp = lane >> 4;
   const SeqRows& s = pl.s;
   const int cap = c.max_pages << c.page_log2;
-  // The last tiles of a prompt see most: they go first.
-  const int nrows = s.n * c.G, ntiles = uniform((nrows + k.tile - 1) / k.tile);
-  const int tile = pl.ranges > 1 ? pl.tile : ntiles - 1 - pl.tile;
   const int row0 = tile * k.tile, wrow0 = row0 + wave * WR;
   const int first = s.p0 + uniform(row0 / c.G), last = s.p0 + uniform((min(row0 + k.tile, nrows) - 1) / c.G);
   const int end = min(max(last + 1, 0), cap);

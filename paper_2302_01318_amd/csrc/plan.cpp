@@ -290,13 +290,13 @@ PagedClass paged_class(const sps_paged_config& c, int tile, int target, long til
   tiles *= c.n_kv_heads;
   const long blocks = (static_cast<long>(c.max_pages) * c.page_size) / 32;
   const long ranges = (blocks + kPagedMinBlocks - 1) / kPagedMinBlocks;
-  // Up to kMaxFew sequences, splitting stops at kPagedMostItems x target items
-  // (unsplit there is one a tile). With more, a sequence of n blocks has at
+  // Up to kMaxFew sequences, splitting stops at kPagedMostItems x target items,
+  // or behind whole rounds of unsplit tiles at target items. With more, a sequence of n blocks has at
   // most n / per + 1 ranges and per is at least (all tiles' blocks) / target:
   // at most target ranges plus one a tile, and the tiles of two ranges or more
   // have at most twice their n / per.
   const long most = static_cast<long>(kPagedMostItems) * target;
-  k.items = std::min(tiles * ranges, c.B <= kMaxFew ? std::max(tiles, most) : tiles + target);
+  k.items = std::min(tiles * ranges, c.B > kMaxFew ? tiles + target : tiles < target ? most : (tiles / target + 1) * target);
   k.slots = ranges > 1 ? std::min(k.items, most) : 0;
   k.o_off = *at;
   *at = align256(*at + static_cast<size_t>(k.slots) * tile * c.head_dim * 4);

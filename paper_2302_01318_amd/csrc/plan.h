@@ -193,7 +193,8 @@ sps_status check_paged_rows(const sps_paged_config& c, bool ragged, int rows, in
 // (a sequence's tokens x the query heads of one KV head) against a range of
 // 32-position blocks. Ranges are the same number of blocks for all sequences
 // of a class, chosen on the device from the actual lengths for the `target`
-// work-groups that the card holds at once. Items whose rows
+// work-groups that the card holds at once; tiles that fill whole rounds of them
+// may stay unsplit. Items whose rows
 // have only one range write the output; the others leave partials in at most
 // `slots` slots of the workspace, which a second launch joins. Sequences with
 // up to `limit` query rows are one class (their waves take different

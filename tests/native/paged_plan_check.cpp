@@ -11,6 +11,7 @@
 #include <cmath>
 #include <cstdio>
 #include <random>
+#include <utility>
 #include <vector>
 
 #include "../../paper_2302_01318_amd/csrc/plan.h"
@@ -33,13 +34,15 @@ struct Seq {
   long tiles, blocks;
 };
 
-// Items and slots per KV head with `per` blocks to a range.
-static void count(const std::vector<Seq>& s, long per, long* items, long* slots) {
+// Items and slots per KV head with the first `whole` tiles unsplit and `per`
+// blocks to a range of the others.
+static void count(const std::vector<Seq>& s, long whole, long per, long* items, long* slots) {
   *items = *slots = 0;
   for (const Seq& q : s) {
-    const long ranges = std::max(1L, (q.blocks + per - 1) / per);
-    *items += q.tiles * ranges;
-    if (ranges > 1) *slots += q.tiles * ranges;
+    const long ranges = std::max(1L, (q.blocks + per - 1) / per), kept = std::min(whole, q.tiles);
+    whole -= kept;
+    *items += kept + (q.tiles - kept) * ranges;
+    if (ranges > 1) *slots += (q.tiles - kept) * ranges;
   }
 }
 
@@ -53,25 +56,24 @@ static void check_class(const sps_paged_config& c, const PagedClass& k, const st
     }
   if (!tiles) return;
   CHECK(k.items > 0, "%s: rows but no grid", name);
-  std::vector<long> choices;
+  std::vector<std::pair<long, long>> choices;                           // (whole, per)
   if (c.B > kMaxFew) {
-    choices.push_back(std::max<long>(kPagedMinBlocks,
-                                     static_cast<long>(std::ceil(static_cast<double>(work) * c.n_kv_heads / k.target))));
+    choices.push_back({0, std::max<long>(kPagedMinBlocks, static_cast<long>(std::ceil(static_cast<double>(work) *
+                                                                                      c.n_kv_heads / k.target)))});
   } else {
-    for (long n = 1; n <= 64; ++n) {
-      const long per = std::max<long>(kPagedMinBlocks, (most + n - 1) / n);
-      long items, slots;
-      count(s, per, &items, &slots);
-      if (n == 1 || items * c.n_kv_heads <= static_cast<long>(kPagedMostItems) * k.target) choices.push_back(per);
-    }
-    // What is taken if none of the prices is a number.
-    long items, slots;
-    count(s, kPagedMinBlocks, &items, &slots);
-    if (most <= kPagedMinBlocks) choices.push_back(kPagedMinBlocks);
+    const long rounds = tiles * c.n_kv_heads / k.target;
+    for (long whole : {0L, rounds * k.target / c.n_kv_heads})
+      for (long n = 1; n <= 64; ++n) {
+        const long per = std::max<long>(kPagedMinBlocks, (most + n - 1) / n);
+        long items, slots;
+        count(s, whole, per, &items, &slots);
+        if ((n == 1 && !whole) || (items - whole) * c.n_kv_heads <= static_cast<long>(whole ? 1 : kPagedMostItems) * k.target)
+          choices.push_back({whole, per});
+      }
   }
-  for (long per : choices) {
+  for (const auto& [whole, per] : choices) {
     long items, slots;
-    count(s, per, &items, &slots);
+    count(s, whole, per, &items, &slots);
     CHECK(items * c.n_kv_heads <= k.items, "%s: %ld items x %d, grid %ld (B %d, per %ld)", name, items, c.n_kv_heads,
           k.items, c.B, per);
     CHECK(slots * c.n_kv_heads <= k.slots, "%s: %ld slots x %d, have %ld (B %d, per %ld)", name, slots, c.n_kv_heads,

@@ -243,6 +243,50 @@ def test_chunks_over_long_contexts_are_split(sps):
         assert torch.equal(again, t.out) and torch.equal(al, t.lse)
 
 
+@pytest.mark.parametrize("dtype, hq, hkv, D, prior, new, window", [
+    ("bf16", 200, 200, 64, [1500, 1571, 1400], [50, 50, 50], 0),
+    ("bf16", 40, 40, 128, [1500], [1700], 0),
+    ("bf16", 80, 40, 64, [1700], [810], 1300),
+    ("bf16", 64, 8, 64, [1500, 40, 900], [1100, 3, 1], 0),
+    ("f32", 40, 40, 64, [1500], [1700], 0),
+    ("f32", 100, 100, 128, [1900, 0, 2100, 1700], [270, 33, 140, 70], 0)])
+def test_tiles_past_whole_rounds_are_split(sps, dtype, hq, hkv, D, prior, new, window):
+    """More tiles than the card holds at once, by a part of a round: the first
+    stay whole, the last are split and joined. fp64 on the device."""
+    t = Batch(sps, dtype, hq, hkv, D, 64, prior, new, seed=21)
+    G, L = hq // hkv, [p + n for p, n in zip(prior, new)]
+    k, v = randn((sum(L), hkv, D), 1, dtype).cuda(), randn((sum(L), hkv, D), 2, dtype).cuda()
+    t.kv.lengths.zero_()
+    at = np.concatenate([[0], np.cumsum(L)]).astype(np.int32)
+    t.kv.append(0, k, v, starts=torch.from_numpy(at).cuda(), max_tokens=max(L))
+    t.kv.lengths.copy_(torch.tensor(prior, dtype=torch.int32))
+    t.attend(window)
+    first, first_lse = t.out.clone(), t.lse.clone()
+    scale = float(np.float32(D ** -0.5))
+    for b, n in enumerate(new):
+        rows = slice(int(t.starts[b]), int(t.starts[b]) + n)
+        pos = prior[b] + torch.arange(n, device="cuda")[:, None]
+        p = torch.arange(L[b], device="cuda")[None, :]
+        seen = (p <= pos) & ((p > pos - window) if window else (p >= 0))
+        for h in range(hkv):
+            K, V = k[at[b]:at[b + 1], h].double(), v[at[b]:at[b + 1], h].double()
+            for g in range(G):
+                q = t.q[rows, h * G + g].double()
+                w = (q @ K.T * scale).masked_fill(~seen, -torch.inf)
+                z = torch.logsumexp(w, 1)
+                w = torch.exp(w - z[:, None])
+                o, W = w @ V, w @ V.abs()
+                M = (q.abs() @ K.abs().T * scale).amax(1)
+                e = (D + 8) * 2.0 ** -24 * M + 2.0 ** -22
+                u = U[dtype]
+                lim = u * o.abs() + (u + 2 * e[:, None] + 2 * L[b] * 2.0 ** -24) * W
+                assert bool(((t.out[rows, h * G + g].double() - o).abs() <= lim).all())
+                dz = (t.lse[rows, h * G + g].double() - z).abs()
+                assert bool((dz <= e + L[b] * 2.0 ** -24 + 2.0 ** -23 * z.abs()).all())
+    t.attend(window)
+    assert torch.equal(t.out, first) and torch.equal(t.lse, first_lse)
+
+
 @pytest.mark.parametrize("seed", range(24))
 def test_attention_of_drawn_batches(sps, seed):
     g = np.random.default_rng(1000 + seed)
