@@ -4,7 +4,7 @@
 // work-group computes the cosines and sines of its rows once, in LDS, and its
 // heads share them. Measured: rope of 8192 x 64 x 128 bf16 54 us, 5.0 TB/s read
 // and written (a plain copy reaches 5.1); append of five chunks, 5189 tokens
-// with 32 heads on 8, 36 us against 25 at that rate; of single tokens both are a
+// with 32 heads on 8, 33 us against 25 at that rate; of single tokens both are a
 // launch (3.6 us, and 7 with the 64 sequences' search for their blocks).
 #include <algorithm>
 #include <cmath>
@@ -175,18 +175,20 @@ hipError_t launch_rope(int dtype, const void* x, int64_t ldx, const int32_t* pos
 }
 
 // One work-group per (32-position block of a sequence's new tokens, KV head):
-// the queries of its heads rotated in passing, its keys rotated into LDS, its
-// values copied there, and both written out in the tiles' order: a 16-byte run
+// its keys rotated into LDS, the queries of its heads rotated in passing, its
+// values copied over the keys once these are out, and both written in the tiles' order: a 16-byte run
 // of keys is 8 dims of a position, one of values 8 positions of a dim (whole
-// ones where the tokens cover them, else element by element).
+// ones where the tokens cover them, else element by element). One LDS tile for
+// both leaves room for six work-groups a CU in bf16 (1368 of them for 5189
+// tokens 32.9 us, 35.5 with a tile each and four a CU).
 template <typename T>
-__global__ __launch_bounds__(256) void paged_append_kernel(PagedView c, PagedRows r, const T* __restrict__ k,
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 6 : 4) void paged_append_kernel(PagedView c, PagedRows r, const T* __restrict__ k,
                                                            int64_t ldk, const T* __restrict__ v, int64_t ldv,
                                                            RopeArgs ra, const T* q, int64_t ldq, T* qo, int64_t ldqo,
                                                            int* err) {
   constexpr int kPad = 8;                          // elements behind a row, against bank conflicts
   __shared__ __align__(16) float2 cs[32 * 64];
-  __shared__ __align__(16) T sk[32 * (128 + kPad)], sv[32 * (128 + kPad)];
+  __shared__ __align__(16) T tile[32 * (128 + kPad)];   // keys, then values
   int* words = reinterpret_cast<int*>(cs);         // blocks of every sequence, before the cosines
   const int lane = threadIdx.x & 63, h = blockIdx.y;
   auto blocks_of = [&](int b) {
@@ -238,15 +240,10 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedView c, PagedRow
   if (c.B > 64) __syncthreads();                   // `words` have been read
   fill_cs(ra, n, [&](int row) { return s.p0 + j0 + row; }, cs);
   __syncthreads();
-  if (page >= 0) rotate_rows<4>(k + row0 * ldk + h * DH, ldk, n, 1, DH, ra, cs, 1.f, sk, ld);
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int i = threadIdx.x + j * 256, row = i / static_cast<uint32_t>(runs), d = (i - row * runs) * 8;
-    if (i < n * runs) *reinterpret_cast<Frag<T>*>(sv + row * ld + d) = vr[j];
-  }
+  if (page >= 0) rotate_rows<4>(k + row0 * ldk + h * DH, ldk, n, 1, DH, ra, cs, 1.f, tile, ld);
+  __syncthreads();
   if (q)
     rotate_rows<4>(q + row0 * ldq + h * c.G * DH, ldq, n, c.G, DH, ra, cs, 1.f, qo + row0 * ldqo + h * c.G * DH, ldqo);
-  __syncthreads();
   if (page < 0) return;
   const size_t area = static_cast<size_t>(DH) << c.page_log2;
   const int in = pos0 & ((1 << c.page_log2) - 1);
@@ -257,8 +254,15 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedView c, PagedRow
   for (int i = threadIdx.x; i < 32 * runs; i += blockDim.x) {
     const int w = (i >= 16 * runs ? 16 : 0) + (i & 15), g = (i >> 4) & (runs - 1);
     if (w >= w0 && w < w0 + n)
-      *reinterpret_cast<Frag<T>*>(kd + i * 8) = *reinterpret_cast<const Frag<T>*>(sk + (w - w0) * ld + g * 8);
+      *reinterpret_cast<Frag<T>*>(kd + i * 8) = *reinterpret_cast<const Frag<T>*>(tile + (w - w0) * ld + g * 8);
   }
+  __syncthreads();                                 // the keys have been read
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int i = threadIdx.x + j * 256, row = i / static_cast<uint32_t>(runs), d = (i - row * runs) * 8;
+    if (i < n * runs) *reinterpret_cast<Frag<T>*>(tile + row * ld + d) = vr[j];
+  }
+  __syncthreads();
   // Values: run i is dim (i / 64) * 16 + i % 16, places 4 g + e and 16 + 4 g + e with g = i / 16 % 4.
   for (int i = threadIdx.x; i < 4 * DH; i += blockDim.x) {
     const int d = (i >> 6) * 16 + (i & 15), g = (i >> 4) & 3;
@@ -269,7 +273,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedView c, PagedRow
       const int w = (e >> 2) * 16 + g * 4 + (e & 3) - w0;
       const bool there = w >= 0 && w < n;
       whole &= there;
-      f.v[e] = sv[(there ? w : 0) * ld + d];
+      f.v[e] = tile[(there ? w : 0) * ld + d];
     }
     if (whole) {
       *reinterpret_cast<Frag<T>*>(vd + i * 8) = f;
