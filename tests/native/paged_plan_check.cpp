@@ -1,4 +1,4 @@
-// Host-only checker of the paged attention's plan (csrc/plan.cpp), built with
+// Holds the paged attention's host-side plan (csrc/plan.cpp) against the device; built with
 // g++ under AddressSanitizer and UndefinedBehaviorSanitizer by
 // tests/test_paged_plan_host.py. The device chooses from the lengths how many
 // blocks a range has; for drawn shapes, lengths and chunks it repeats the
