@@ -25,7 +25,7 @@
 //   1 token at position 2048, 32 heads on 32                   14 us (launches)
 //   16 x 5 tokens at 4.5 to 8 thousand, 64 heads on 8          92 us, 4.8 TB/s
 //   4 x 1 tokens at 105 to 126 thousand, 32 heads on 8        284 us, 6.6 TB/s
-//   a prompt of 8192 tokens, 32 heads on 8                    540 us, 1.02 PFLOP/s
+//   a prompt of 8192 tokens, 32 heads on 8                    540 us, 1.02 PFLOP/s (574 on another card)
 //   1297 tokens of 27 sequences (three of 264 to 665), 64
 //     heads on 8, over windows of 4096 positions              293 us
 // fp32: 2 x 5 tokens at 64 to 79 positions 7 us, a launch.

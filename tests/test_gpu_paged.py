@@ -230,6 +230,35 @@ def test_many_sequences(sps):
     t.check()
 
 
+@pytest.mark.parametrize("dtype, B, window", [("bf16", 65, 0), ("bf16", 130, 100), ("f32", 90, 0), ("bf16", 64, 0)])
+def test_many_sequences_of_both_kinds(sps, dtype, B, window):
+    """Prompt chunks, drafts, single tokens and waiting requests, some of them
+    over long contexts, around the number of sequences whose split is priced."""
+    g = np.random.default_rng(B)
+    prior, new = g.integers(0, 300, B).tolist(), [(1, 5, 0, 1, 2)[b % 5] for b in range(B)]
+    for b, (p, n) in {0: (3000, 1), 3: (10, 70), 40: (900, 33), B - 1: (2500, 9)}.items():
+        prior[b], new[b] = p, n
+    t = Batch(sps, dtype, 8, 2, 64, 32, prior, new, seed=22, extra_rows=2, before=1)
+    t.attend(window)
+    t.check(window)
+    assert sps.device_error() == 0
+
+
+def test_two_streams_at_once(sps):
+    """Calls that overlap on two streams, each with its workspace, over one cache."""
+    t = Batch(sps, "bf16", 16, 2, 128, 64, [9000, 4000, 700], [1, 40, 5], seed=23)
+    ws = [t.kv.workspace(t.rows, t.most) for _ in range(2)]
+    want = t.attend(lse=False).clone()
+    outs, streams = [torch.empty_like(t.out) for _ in range(2)], [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for s in range(2):
+            with torch.cuda.stream(streams[s]):
+                sps.paged_attention(t.kv, 0, t.q, ws[s], out=outs[s], starts=t.st, max_tokens=t.most)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
+
+
 def test_chunks_over_long_contexts_are_split(sps):
     """Tiles of many rows with several ranges, joined; with a window, and among
     more sequences than the ranges are priced for."""
