@@ -291,10 +291,10 @@ PagedClass paged_class(const sps_paged_config& c, int tile, int target, long til
   const long blocks = (static_cast<long>(c.max_pages) * c.page_size) / 32;
   const long ranges = (blocks + kPagedMinBlocks - 1) / kPagedMinBlocks;
   // Up to kMaxFew sequences, splitting stops at kPagedMostItems x target items,
-  // or behind whole rounds of unsplit tiles at target items. With more, a sequence of n blocks has at
-  // most n / per + 1 ranges and per is at least (all tiles' blocks) / target:
-  // at most target ranges plus one a tile, and the tiles of two ranges or more
-  // have at most twice their n / per.
+  // or behind whole rounds of unsplit tiles at target items. With more, a
+  // sequence of n blocks has at most n / per + 1 ranges and per is at least
+  // (all tiles' blocks) / target: at most target ranges plus one a tile, and the
+  // tiles of two ranges or more have at most twice their n / per.
   const long most = static_cast<long>(kPagedMostItems) * target;
   k.items = std::min(tiles * ranges, c.B > kMaxFew ? tiles + target : tiles < target ? most : (tiles / target + 1) * target);
   k.slots = ranges > 1 ? std::min(k.items, most) : 0;
